@@ -421,6 +421,93 @@ fpq_status fpq_round_learn_unfold(const float* x, int32_t B, int32_t C, int32_t 
 fpq_status fpq_round_learn_harden(const float* alpha, int64_t N, int64_t K, uint8_t* rounding_bits, void* stream);
 
 /*
+ * Low-rank adapters of many requests at once, beside a shared projection: the call behind a quantized layer whose
+ * output it takes as `base`.  Row i of segment s (rows offsets[s] .. offsets[s + 1]) uses adapter g = ids[s]:
+ *     u[i] = A[g] x[i],     y[i] = base[i] + scale[g] * B[g] u[i]
+ * A segment whose id is negative or not below G has no adapter: y[i] = base[i], u[i] = 0.  Rows in no segment (in front
+ * of offsets[0], behind offsets[S]) are neither read nor written.
+ *   x        [M][K] of x_type, rows ldx elements apart (ldx >= K); base and y [M][N] of x_type likewise.  base may be NULL
+ *            (zeros) and may be y itself (same rows, same ld); nothing else may overlap what is written
+ *   a, b     A [G][R][K] and B [G][N][R] of w_type, contiguous, 1 <= R <= 128 (adapters of lower rank: rows of zeros)
+ *   x_type   FPQ_FP32, FPQ_BF16 or FPQ_FP16; w_type any of them for FPQ_FP32, else the same (FPQ_ERR_UNSUPPORTED)
+ *   scale    [G] FP32 or NULL (ones)
+ *   offsets  [S + 1] int32, non-decreasing (values outside 0 .. M are clamped: a wrong list gives wrong rows, no access
+ *            out of range); ids [S] int32.  One adapter may serve any number of segments; segments may be empty
+ *   u        NULL, or [M][R] FP32 out: what fpq_adapter_backward reads
+ * Sums are FP32: FP32 operands enter the tensor cores as two TF32 terms each (errors of 2^-22 of the sum of absolute
+ * terms, as FP32 multiply-adds have), 16-bit operands as they are; y is rounded once.  An infinite or NaN operand gives
+ * what FP32 multiply-adds give.  Nothing depends on other rows, and equal calls give equal bits.
+ *
+ * fpq_adapter_backward: the gradients, from dy [M][N] (rows ld_dy apart) and what forward read and kept:
+ *     t[i] = scale[g] * B[g]^T dy[i],   dx[i] = base[i] + A[g]^T t[i],
+ *     da[g] = sum_i t[i] x[i]^T,        db[g] = scale[g] * sum_i dy[i] u[i]^T      over the rows of adapter g's segments
+ *   base     [M][K] of x_type or NULL: the gradient that reaches x on other ways; may be dx itself
+ *   dx       [M][K] out, or NULL when x needs no gradient; rows in no segment stay as they were
+ *   da, db   [G][R][K] and [G][N][R] FP32 out, overwritten (zeros for an adapter without rows).  No atomics: equal calls
+ *            give equal bits
+ *   workspace  fpq_adapter_backward_workspace_size(M, R) bytes, 16-byte aligned, contents not kept
+ * One kernel forward, two backward, on `stream`; no allocation, no synchronisation.  Pointers are aligned to their
+ * element; rows at multiples of 16 bytes are read 16 bytes at a time.  Limits: M and S below 2^31 and 2^24, N and K
+ * up to 2^24, G up to 65535, G * R * max(N, K) below 2^40.  M = 0 or S = 0: forward does nothing, backward writes zeros to
+ * da and db.  Errors: FPQ_ERR_UNSUPPORTED, FPQ_ERR_SHAPE, FPQ_ERR_NULL, FPQ_ERR_ALIGN, FPQ_ERR_WORKSPACE, FPQ_ERR_CUDA.
+ */
+enum { FPQ_FP32 = 0, FPQ_BF16 = 1, FPQ_FP16 = 2, FPQ_E4M3_BLOCK32 = 3 };
+fpq_status fpq_adapter_forward(const void* x, int64_t ldx, int32_t x_type, const void* a, const void* b, int32_t w_type,
+                               const float* scale, int32_t G, int32_t R, const int32_t* offsets, const int32_t* ids, int32_t S,
+                               const void* base, int64_t ld_base, void* y, int64_t ldy, float* u, int64_t M, int64_t N, int64_t K,
+                               void* stream);
+size_t fpq_adapter_backward_workspace_size(int64_t M, int32_t R);
+fpq_status fpq_adapter_backward(const void* dy, int64_t ld_dy, const void* x, int64_t ldx, int32_t x_type, const float* u,
+                                const void* a, const void* b, int32_t w_type, const float* scale, int32_t G, int32_t R,
+                                const int32_t* offsets, const int32_t* ids, int32_t S, const void* base, int64_t ld_base, void* dx,
+                                int64_t ld_dx, float* da, float* db, int64_t M, int64_t N, int64_t K, void* workspace,
+                                size_t ws_bytes, void* stream);
+
+/*
+ * One AdamW step over many tensors (adapters, or the alpha of the learned rounding with the gradient of
+ * fpq_round_learn_step), with decoupled weight decay; t is the number of this step, from 1:
+ *     g' = factors[1] g,  m = beta1 m + (1 - beta1) g',  v = beta2 v + (1 - beta2) g'^2,  rate = factors[0] lr
+ *     p = p (1 - rate weight_decay) - rate / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ *   tensors_host  HOST array of count descriptors (read during the call): p [n] FP32 updated in place, g [n] of g_type
+ *            (FPQ_FP32, FPQ_BF16, FPQ_FP16), m and v [n] updated in place, copy: NULL or [n] of copy_type (FPQ_BF16 or
+ *            FPQ_FP16) that receives the new p rounded once.  n = 0 is allowed.  No two buffers may overlap.
+ *   state_type  FPQ_FP32: m and v are FP32, m_scale and v_scale are not used;
+ *            FPQ_E4M3_BLOCK32: m and v are E4M3 codes (bias 7) of the first moment and of the SQUARE ROOT of the second,
+ *            m_scale and v_scale [ceil(n / 32)] bytes b, each the scale 2^(b - 127) of 32 codes (value = code * scale).
+ *            Zeroed buffers are the state before the first step.  p is updated with the moments before they are rounded
+ *            to codes; the scale brings a block's largest finite magnitude into [128, 256), codes are rounded
+ *            stochastically: up if the remainder below a code's step, as 20 bits, plus 16 noise bits at their top
+ *            carries.  A positive square root keeps the code 1 at least; a value that is not finite gets the code 0x7F
+ *            (NaN).  With mix(z): z = z * 0x9E3779B1, z ^= z >> 15, z = z * 0x243F6A89, z ^= z >> 16 (32 bits), element
+ *            number e (each tensor starts at the next multiple of 32 behind the one in front) has
+ *            mix(low(e) ^ mix(t * 0x9E3779B1 + seed + 1 + high(e) * 0x243F6A89)); its upper half is m's noise, its lower
+ *            half the square root's
+ *   options_host  lr, weight_decay finite; beta1, beta2 in [0, 1); eps finite and not negative
+ *   factors  NULL (ones) or DEVICE float[2]: what a schedule or a gradient clip changes between replays of a captured call
+ *   step     DEVICE int64[2] {steps made, 0}, advanced by the call; the second entry is scratch, zero before and after
+ * One kernel per 400 tensors on `stream`.  Errors: FPQ_ERR_UNSUPPORTED (types), FPQ_ERR_SHAPE (count or n negative, n or
+ * their sum not below 2^40, options out of range), FPQ_ERR_NULL, FPQ_ERR_ALIGN (pointers to their element; step 8 bytes),
+ * FPQ_ERR_CUDA.
+ */
+typedef struct {
+    float* p;
+    const void* g;
+    void* m;
+    void* v;
+    uint8_t* m_scale;
+    uint8_t* v_scale;
+    void* copy;
+    int64_t n;
+} fpq_adamw_tensor;
+typedef struct {
+    double lr, beta1, beta2, eps, weight_decay;
+    uint32_t seed, reserved;
+} fpq_adamw_options;
+fpq_status fpq_adamw_step(const fpq_adamw_tensor* tensors_host, int32_t count, int32_t g_type, int32_t copy_type,
+                          int32_t state_type, const fpq_adamw_options* options_host, const float* factors, int64_t* step,
+                          void* stream);
+
+/*
  * Which route fpq_linear / fpq_conv2d take (process-wide setting, not thread-safe against
  * concurrent layer calls).  Every route multiplies the same codes exactly and adds in FP32, so the
  * results agree within the layer tolerance; routes that run the same MMAs in the same order agree

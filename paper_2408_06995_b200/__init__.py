@@ -2,9 +2,9 @@
 
 Every function here has the name of the C entry point it calls
 (include/fpq.h) and passes torch tensors' device pointers and the current CUDA
-stream: the calls a running model makes per layer, the encoding search and the
-rounding-learning step through a small CPython extension (csrc/fpq_torch.cpp),
-the others through ctypes.  All arithmetic runs
+stream: the calls a running model makes per layer, the encoding search, the
+rounding-learning step, the adapters and the AdamW step through a small CPython
+extension (csrc/fpq_torch.cpp), the others through ctypes.  All arithmetic runs
 in the library's kernels.  There is no fallback: if the shared library is
 missing the import of a symbol fails.
 """
@@ -29,6 +29,7 @@ CONTRACTION_GENERAL, CONTRACTION_PAIRS, CONTRACTION_CUDA_CORES, CONTRACTION_OTHE
 STATIC_SCRATCH_BYTES = 8 << 20
 SAT_PAPER, SAT_NATIVE = 0, 1
 LINEAR, CONV2D = 0, 1
+FP32, BF16, FP16, E4M3_BLOCK32 = 0, 1, 2, 3
 PATH_AUTO, PATH_FUSED, PATH_TWO_KERNELS, PATH_TWO_KERNELS_NARROW = 0, 1, 2, 3
 
 
@@ -80,6 +81,7 @@ EXPORTS = [
     "fpq_zero_census", "fpq_prepared_size_split", "fpq_prepare_weight_split", "fpq_conv2d_split_workspace_size",
     "fpq_conv2d_split", "fpq_set_path_policy", "fpq_get_path_policy", "fpq_read_status", "fpq_status_string",
     "fpq_conv2d_route", "fpq_linear_contraction", "fpq_conv2d_contraction", "fpq_selftest_bounded_wait",
+    "fpq_adapter_forward", "fpq_adapter_backward_workspace_size", "fpq_adapter_backward", "fpq_adamw_step",
 ]
 
 _lib = None
@@ -167,6 +169,15 @@ def lib() -> ctypes.CDLL:
         L.fpq_linear_contraction.argtypes = [i64, i64, i64, F, F]
         L.fpq_conv2d_contraction.restype = i32
         L.fpq_conv2d_contraction.argtypes = [i32] * 9 + [F, F]
+        L.fpq_adapter_forward.restype = i32
+        L.fpq_adapter_forward.argtypes = [vp, i64, i32, vp, vp, i32, vp, i32, i32, vp, vp, i32, vp, i64, vp, i64, vp, i64, i64, i64, vp]
+        L.fpq_adapter_backward_workspace_size.restype = sz
+        L.fpq_adapter_backward_workspace_size.argtypes = [i64, i32]
+        L.fpq_adapter_backward.restype = i32
+        L.fpq_adapter_backward.argtypes = [vp, i64, vp, i64, i32, vp, vp, vp, i32, vp, i32, i32, vp, vp, i32, vp, i64, vp, i64, vp, vp,
+                                           i64, i64, i64, vp, sz, vp]
+        L.fpq_adamw_step.restype = i32
+        L.fpq_adamw_step.argtypes = [vp, i32, i32, i32, i32, vp, vp, vp, vp]
         L.fpq_read_status.restype = i32
         L.fpq_read_status.argtypes = [vp]
         L.fpq_status_string.restype = ctypes.c_char_p
@@ -467,6 +478,118 @@ def fpq_round_learn_harden(alpha: torch.Tensor, bits: torch.Tensor = None) -> to
         bits = torch.empty((N, (K + 7) // 8), dtype=torch.uint8, device=alpha.device)
     _check(lib().fpq_round_learn_harden(_ptr(alpha), N, K, _ptr(bits), _stream()), "fpq_round_learn_harden")
     return bits
+
+
+def fpq_adapter_forward(x: torch.Tensor, a: torch.Tensor, b: torch.Tensor, offsets: torch.Tensor, ids: torch.Tensor, scale=None, base=None,
+                        y: torch.Tensor = None, u: torch.Tensor = None) -> torch.Tensor:
+    """y[i] = base[i] + scale[g] B[g] (A[g] x[i]) for the rows i of segment s, g = ids[s].  x [M][K], base and y [M][N] of float32,
+    bfloat16 or float16 (rows may lie apart); a [G][R][K], b [G][N][R]; offsets int32 [S + 1], ids int32 [S].  base may be y; without y a
+    new one is made, in which rows outside of the segments are base's (zeros without a base).  u: None, or [M][R] float32 that
+    receives A[g] x[i], which the backward pass reads."""
+    if y is None:
+        y = base.clone(memory_format=torch.contiguous_format) if base is not None else x.new_zeros((x.shape[0], b.shape[1]))
+    code = (_layers or _load_layers()).adapter_forward(x, a, b, offsets, ids, scale, base, y, u)
+    if code:
+        raise FpqError(code, "fpq_adapter_forward")
+    return y
+
+
+def fpq_adapter_backward_workspace_size(M: int, R: int) -> int:
+    return lib().fpq_adapter_backward_workspace_size(int(M), int(R))
+
+
+def fpq_adapter_backward(dy: torch.Tensor, x: torch.Tensor, u: torch.Tensor, a: torch.Tensor, b: torch.Tensor, offsets: torch.Tensor,
+                         ids: torch.Tensor, scale=None, base=None, dx: torch.Tensor = None, da: torch.Tensor = None,
+                         db: torch.Tensor = None, workspace: torch.Tensor = None, need_dx: bool = True):
+    """The gradients of fpq_adapter_forward: (dx [M][K] of x's type, or None without need_dx; da [G][R][K] and db [G][N][R] float32).
+    base: the gradient that reaches x on other ways (through the shared projection); it may be dx."""
+    if not need_dx:
+        dx = base = None
+    elif dx is None:
+        dx = base.clone(memory_format=torch.contiguous_format) if base is not None else torch.zeros_like(x, memory_format=torch.contiguous_format)
+    if da is None:
+        da = torch.empty(a.shape, dtype=torch.float32, device=a.device)
+    if db is None:
+        db = torch.empty(b.shape, dtype=torch.float32, device=b.device)
+    if workspace is None:
+        workspace = torch.empty(max(16, fpq_adapter_backward_workspace_size(x.shape[0], a.shape[1])), dtype=torch.uint8, device=x.device)
+    code = (_layers or _load_layers()).adapter_backward(dy, x, u, a, b, offsets, ids, scale, base, dx, da, db, workspace)
+    if code:
+        raise FpqError(code, "fpq_adapter_backward")
+    return dx, da, db
+
+
+class _CAdamwTensor(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_void_p) for name in ("p", "g", "m", "v", "m_scale", "v_scale", "copy")] + [("n", ctypes.c_int64)]
+
+
+class AdamwTable:
+    """The tensors of an AdamW step, laid out as fpq_adamw_step reads them.  It keeps the tensors; their contents may change between
+    steps (gradients are written to the same buffers), their storage may not."""
+
+    def __init__(self, params, grads, m, v, m_scale=None, v_scale=None, copies=None):
+        count = len(params)
+        real = {torch.float32: FP32, torch.bfloat16: BF16, torch.float16: FP16}
+        codes = (torch.uint8, torch.float8_e4m3fn)
+        scales = (torch.uint8, torch.float8_e8m0fnu)
+        given = [list(t) if t is not None else [None] * count for t in (params, grads, m, v, m_scale, v_scale, copies)]
+        assert all(len(t) == count for t in given), "expected lists of one length"
+        params, grads, m, v, m_scale, v_scale, copies = given
+        self.state_type = E4M3_BLOCK32 if count and m[0].dtype in codes else FP32
+        self.g_type = real.get(grads[0].dtype if count else torch.float32, -1)
+        kinds = {t.dtype for t in copies if t is not None}
+        assert len(kinds) <= 1 and kinds <= {torch.bfloat16, torch.float16}, "copies: expected bfloat16 or float16"
+        self.copy_type = real[kinds.pop()] if kinds else BF16
+        self.device = params[0].get_device() if count else None
+        assert self.g_type >= 0, "gradients: expected float32, bfloat16 or float16"
+        self._table = (_CAdamwTensor * count)()
+        written = set()
+
+        def pointer(t, n, dtypes, what, optional=False):
+            if t is None and optional:
+                return None
+            assert t is not None and t.is_cuda and t.get_device() == self.device and t.dtype in dtypes and t.is_contiguous() and t.numel() == n, \
+                f"{what}: expected a contiguous tensor of {n} elements of {' or '.join(map(str, dtypes))} on the parameters' device"
+            return t.data_ptr()
+
+        for i, p in enumerate(params):
+            n, e = p.numel(), self._table[i]
+            blocks = -(-n // 32)
+            e.n = n
+            e.p = pointer(p, n, (torch.float32,), "params")
+            e.g = pointer(grads[i], n, (grads[0].dtype,), "grads")
+            e.copy = pointer(copies[i], n, (torch.bfloat16, torch.float16), "copies", True)
+            if self.state_type == FP32:
+                e.m, e.v = pointer(m[i], n, (torch.float32,), "m"), pointer(v[i], n, (torch.float32,), "v")
+            else:
+                e.m, e.v = pointer(m[i], n, codes, "m"), pointer(v[i], n, codes, "v")
+                e.m_scale, e.v_scale = pointer(m_scale[i], blocks, scales, "m_scale"), pointer(v_scale[i], blocks, scales, "v_scale")
+            if n:
+                mine = [q for q in (e.p, e.m, e.v, e.m_scale, e.v_scale, e.copy) if q]
+                assert len(set(mine)) == len(mine) and written.isdisjoint(mine), "a buffer appears twice"
+                written.update(mine)
+        self._kept = given
+
+
+def fpq_adamw_table(params, grads, m, v, m_scale=None, v_scale=None, copies=None) -> AdamwTable:
+    """The list of tensors for fpq_adamw_step.  params: float32; grads: one type of float32, bfloat16, float16; m, v: float32, or E4M3
+    codes (uint8 or float8_e4m3fn; v holds the square root of the second moment) with m_scale, v_scale, one byte (uint8 or
+    float8_e8m0fnu) per 32 elements; copies: None, or bfloat16 / float16 tensors (or None for some) that receive the new parameters."""
+    return AdamwTable(params, grads, m, v, m_scale, v_scale, copies)
+
+
+def fpq_adamw_step(table: AdamwTable, step: torch.Tensor, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
+                   weight_decay: float = 0.0, seed: int = 0, factors: torch.Tensor = None) -> None:
+    """One AdamW step over the table's tensors, in place.  step: int64 [2] on the device, {steps made, 0}, advanced by the call;
+    factors: None, or float32 [2] on the device {of lr, of the gradients}; seed: of the stochastic rounding of 8-bit moments."""
+    if table.device is None:
+        table_device = step.get_device()
+    else:
+        table_device = table.device
+    code = (_layers or _load_layers()).adamw_step(table._table, table_device, table.g_type, table.copy_type, table.state_type, lr, beta1, beta2,
+                                                  eps, weight_decay, seed, factors, step)
+    if code:
+        raise FpqError(code, "fpq_adamw_step")
 
 
 def fpq_set_path_policy(policy: int) -> None:

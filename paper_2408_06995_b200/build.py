@@ -12,7 +12,7 @@ CSRC = os.path.join(HERE, "csrc")
 SO = os.path.join(HERE, "libfpq.so")
 BINDING = os.path.join(HERE, "_fpq_torch.so")
 SOURCES = ["fpq_api.cu", "fpq_quantize.cu", "fpq_gemm.cu", "fpq_pair.cu", "fpq_pair_gemm.cu", "fpq_pair_rows.cu", "fpq_noalloc.cu", "fpq_search.cu", "fpq_smallm.cu", "fpq_fewrows.cu",
-           "fpq_roundlearn.cu", "fpq_general.cu", "fpq_tf32.cu", "fpq_tensormap.cu"]
+           "fpq_roundlearn.cu", "fpq_general.cu", "fpq_tf32.cu", "fpq_tensormap.cu", "fpq_adapter.cu", "fpq_adamw.cu"]
 
 
 def _newest_source_mtime() -> float:
@@ -26,7 +26,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         return SO
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
-           "-shared", "-Xcompiler", "-fPIC", "-I", os.path.join(ROOT, "include"), "-I", CSRC,
+           "-shared", "--threads", "0", "-Xcompiler", "-fPIC", "-I", os.path.join(ROOT, "include"), "-I", CSRC,
            "-cudart", "static"]
     if verbose:
         cmd += ["-Xptxas", "-v"]

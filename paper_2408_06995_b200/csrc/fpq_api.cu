@@ -1422,6 +1422,132 @@ fpq_status fpq_round_learn_harden(const float* alpha, int64_t N, int64_t K, uint
     return launch_round_harden(alpha, N, K, rounding_bits, (cudaStream_t)stream);
 }
 
+// ---- low-rank adapters and the AdamW step ---------------------------------------------------------
+static size_t real_bytes(int32_t type) { return type == FPQ_FP32 ? 4 : 2; }
+static bool real_type(int32_t type) { return type == FPQ_FP32 || type == FPQ_BF16 || type == FPQ_FP16; }
+
+static fpq_status check_adapters(const AdapterProblem& p)
+{
+    if (!real_type(p.x_type) || !real_type(p.w_type) || (p.x_type != FPQ_FP32 && p.w_type != p.x_type))
+        return FPQ_ERR_UNSUPPORTED;
+    const int64_t most = (int64_t)1 << 24;
+    if (p.M < 0 || p.M > 0x7fffffff || p.S < 0 || p.S > most || p.N < 1 || p.N > most || p.K < 1 || p.K > most || p.G < 1 ||
+        p.G > 65535 || p.R < 1 || p.R > 128 || (int64_t)p.G * p.R * (p.N > p.K ? p.N : p.K) >= ((int64_t)1 << 40))
+        return FPQ_ERR_SHAPE;
+    return FPQ_OK;
+}
+
+static fpq_status check_adapter_pointers(const AdapterProblem& p)
+{
+    if (!p.a || !p.b || !p.offsets || !p.ids)
+        return FPQ_ERR_NULL;
+    const size_t w = real_bytes(p.w_type);
+    if (!aligned(p.a, w) || !aligned(p.b, w) || !aligned(p.scale, 4) || !aligned(p.offsets, 4) || !aligned(p.ids, 4))
+        return FPQ_ERR_ALIGN;
+    return FPQ_OK;
+}
+
+// a matrix of `rows` rows; one row at most needs no distance between rows
+static bool bad_ld(int64_t ld, int64_t width) { return ld < width || ld > ((int64_t)1 << 32); }
+
+fpq_status fpq_adapter_forward(const void* x, int64_t ldx, int32_t x_type, const void* a, const void* b, int32_t w_type,
+                               const float* scale, int32_t G, int32_t R, const int32_t* offsets, const int32_t* ids, int32_t S,
+                               const void* base, int64_t ld_base, void* y, int64_t ldy, float* u, int64_t M, int64_t N, int64_t K,
+                               void* stream)
+{
+    const AdapterProblem p = {a, b, scale, offsets, ids, x_type, w_type, G, R, S, M, N, K};
+    fpq_status s = check_adapters(p);
+    if (s != FPQ_OK)
+        return s;
+    if (bad_ld(ldx, K) || bad_ld(ldy, N) || (base && bad_ld(ld_base, N)))
+        return FPQ_ERR_SHAPE;
+    if (M == 0 || S == 0)
+        return FPQ_OK;
+    if (!x || !y)
+        return FPQ_ERR_NULL;
+    s = check_adapter_pointers(p);
+    if (s != FPQ_OK)
+        return s;
+    const size_t xb = real_bytes(x_type);
+    if (!aligned(x, xb) || !aligned(base, xb) || !aligned(y, xb) || !aligned(u, 4))
+        return FPQ_ERR_ALIGN;
+    return launch_adapter_forward(p, x, ldx, base, ld_base, y, ldy, u, (cudaStream_t)stream) == cudaSuccess ? FPQ_OK : FPQ_ERR_CUDA;
+}
+
+size_t fpq_adapter_backward_workspace_size(int64_t M, int32_t R)
+{
+    if (M < 0 || M > 0x7fffffff || R < 1 || R > 128)
+        return 0;
+    return (size_t)M * (size_t)R * 4 + 16;
+}
+
+fpq_status fpq_adapter_backward(const void* dy, int64_t ld_dy, const void* x, int64_t ldx, int32_t x_type, const float* u,
+                                const void* a, const void* b, int32_t w_type, const float* scale, int32_t G, int32_t R,
+                                const int32_t* offsets, const int32_t* ids, int32_t S, const void* base, int64_t ld_base, void* dx,
+                                int64_t ld_dx, float* da, float* db, int64_t M, int64_t N, int64_t K, void* workspace,
+                                size_t ws_bytes, void* stream)
+{
+    const AdapterProblem p = {a, b, scale, offsets, ids, x_type, w_type, G, R, S, M, N, K};
+    fpq_status s = check_adapters(p);
+    if (s != FPQ_OK)
+        return s;
+    if (bad_ld(ld_dy, N) || bad_ld(ldx, K) || (dx && bad_ld(ld_dx, K)) || (dx && base && bad_ld(ld_base, K)))
+        return FPQ_ERR_SHAPE;
+    if (!da || !db)
+        return FPQ_ERR_NULL;
+    if (!aligned(da, 4) || !aligned(db, 4))
+        return FPQ_ERR_ALIGN;
+    if (M > 0 && S > 0) {
+        if (!dy || !x || !u)
+            return FPQ_ERR_NULL;
+        s = check_adapter_pointers(p);
+        if (s != FPQ_OK)
+            return s;
+        const size_t xb = real_bytes(x_type);
+        if (!aligned(dy, xb) || !aligned(x, xb) || !aligned(dx, xb) || !aligned(base, xb) || !aligned(u, 4) || !aligned(workspace, 16))
+            return FPQ_ERR_ALIGN;
+        if (!workspace || ws_bytes < fpq_adapter_backward_workspace_size(M, R))
+            return FPQ_ERR_WORKSPACE;
+    }
+    return launch_adapter_backward(p, dy, ld_dy, x, ldx, u, dx ? base : nullptr, ld_base, dx, ld_dx, da, db, (float*)workspace,
+                                   (cudaStream_t)stream) == cudaSuccess ? FPQ_OK : FPQ_ERR_CUDA;
+}
+
+fpq_status fpq_adamw_step(const fpq_adamw_tensor* tensors_host, int32_t count, int32_t g_type, int32_t copy_type,
+                          int32_t state_type, const fpq_adamw_options* options_host, const float* factors, int64_t* step,
+                          void* stream)
+{
+    if (!real_type(g_type) || (copy_type != FPQ_BF16 && copy_type != FPQ_FP16) ||
+        (state_type != FPQ_FP32 && state_type != FPQ_E4M3_BLOCK32))
+        return FPQ_ERR_UNSUPPORTED;
+    if (count < 0)
+        return FPQ_ERR_SHAPE;
+    if (!options_host || !step || (count > 0 && !tensors_host))
+        return FPQ_ERR_NULL;
+    const fpq_adamw_options& o = *options_host;
+    if (!std::isfinite(o.lr) || !std::isfinite(o.weight_decay) || !std::isfinite(o.eps) || o.eps < 0 || !(o.beta1 >= 0 && o.beta1 < 1) ||
+        !(o.beta2 >= 0 && o.beta2 < 1))
+        return FPQ_ERR_SHAPE;
+    if (!aligned(step, 8) || !aligned(factors, 4))
+        return FPQ_ERR_ALIGN;
+    const bool codes = state_type == FPQ_E4M3_BLOCK32;
+    const int64_t most = (int64_t)1 << 40;
+    int64_t total = 0;
+    for (int32_t i = 0; i < count; ++i) {
+        const fpq_adamw_tensor& t = tensors_host[i];
+        if (t.n < 0 || t.n >= most || (total += t.n) >= most)
+            return FPQ_ERR_SHAPE;
+        if (t.n == 0)
+            continue;
+        if (!t.p || !t.g || !t.m || !t.v || (codes && (!t.m_scale || !t.v_scale)))
+            return FPQ_ERR_NULL;
+        if (!aligned(t.p, 4) || !aligned(t.g, real_bytes(g_type)) || !aligned(t.copy, 2) ||
+            (!codes && (!aligned(t.m, 4) || !aligned(t.v, 4))))
+            return FPQ_ERR_ALIGN;
+    }
+    return launch_adamw(tensors_host, count, g_type, copy_type, state_type, o, factors, step, (cudaStream_t)stream);
+}
+
 int32_t fpq_conv2d_route(int B, int C, int H, int W, int C_out, int R, int S, int pad, int stride, fpq_format fx,
                          fpq_format fw)
 {

@@ -167,4 +167,20 @@ struct GeneralLayer {
 size_t general_layer_workspace_bytes(const GeneralLayer& g);
 fpq_status launch_general_layer(const GeneralLayer& g, void* workspace, cudaStream_t st);
 
+// Low-rank adapters (t: [M][R] scratch that receives s B^T dy), and the AdamW step; arguments checked by the callers.
+struct AdapterProblem {
+    const void *a, *b;        // [G][R][K], [G][N][R]
+    const float* scale;       // [G] or NULL
+    const int32_t *offsets, *ids;
+    int x_type, w_type, G, R, S;
+    int64_t M, N, K;
+};
+cudaError_t launch_adapter_forward(const AdapterProblem& p, const void* x, int64_t ldx, const void* base, int64_t ld_base, void* y,
+                                   int64_t ldy, float* u, cudaStream_t st);
+cudaError_t launch_adapter_backward(const AdapterProblem& p, const void* dy, int64_t ld_dy, const void* x, int64_t ldx, const float* u,
+                                    const void* base, int64_t ld_base, void* dx, int64_t ld_dx, float* da, float* db, float* t,
+                                    cudaStream_t st);
+fpq_status launch_adamw(const fpq_adamw_tensor* t, int count, int g_type, int copy_type, int state_type, const fpq_adamw_options& o,
+                        const float* factors, int64_t* step, cudaStream_t st);
+
 }  // namespace fpq

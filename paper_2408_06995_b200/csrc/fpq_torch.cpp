@@ -7,6 +7,9 @@
 // well under 1 us.
 #include <Python.h>
 
+#include <initializer_list>
+
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -295,12 +298,213 @@ PyObject* learn_step(PyObject*, PyObject* const* a, Py_ssize_t n)
     return PyLong_FromLong(status);
 }
 
+// ---- low-rank adapters and the AdamW step: tensors of several types with strides between rows, all on the current device
+
+// what a call reads or writes: None gives a null pointer where that is allowed
+struct Matrix {
+    void* p = nullptr;
+    int type = -1;                 // FPQ_FP32, FPQ_BF16, FPQ_FP16
+    int64_t rows = 0, cols = 0, ld = 0;
+};
+
+bool wrong(const char* what)
+{
+    PyErr_SetString(PyExc_AssertionError, what);
+    return false;
+}
+
+int real_type(at::ScalarType t)
+{
+    return t == at::kFloat ? FPQ_FP32 : t == at::kBFloat16 ? FPQ_BF16 : t == at::kHalf ? FPQ_FP16 : -1;
+}
+
+// every tensor lies on the device that is current: the call's kernels and its stream are that one's
+bool on_device(const at::Tensor& t) { return t.is_cuda() && t.get_device() == c10::cuda::current_device(); }
+
+// [rows][cols], columns side by side, rows at any distance that keeps them apart
+bool matrix(PyObject* o, bool none, Matrix* m, const char* what)
+{
+    if (o == Py_None && none)
+        return true;
+    bool fits = false;
+    if (THPVariable_Check(o) && !guarded([&] {
+            const at::Tensor& t = THPVariable_Unpack(o);
+            if (!on_device(t) || t.dim() != 2)
+                return;
+            m->type = real_type(t.scalar_type());
+            m->rows = t.size(0);
+            m->cols = t.size(1);
+            m->ld = m->rows > 1 ? t.stride(0) : m->cols;
+            fits = m->type >= 0 && (m->cols <= 1 || t.stride(1) == 1) && m->ld >= m->cols;
+            m->p = t.data_ptr();
+        }))
+        return false;
+    return fits || wrong(what);
+}
+
+// a contiguous tensor of one scalar type and shape; sizes of -1 are taken as they are and given back
+bool array(PyObject* o, bool none, at::ScalarType type, std::initializer_list<int64_t*> sizes, void** p, const char* what)
+{
+    *p = nullptr;
+    if (o == Py_None && none)
+        return true;
+    bool fits = false;
+    if (THPVariable_Check(o) && !guarded([&] {
+            const at::Tensor& t = THPVariable_Unpack(o);
+            if (!on_device(t) || t.scalar_type() != type || !t.is_contiguous() || t.dim() != (int64_t)sizes.size())
+                return;
+            int64_t i = 0;
+            fits = true;
+            for (int64_t* want : sizes) {
+                if (*want < 0)
+                    *want = t.size(i);
+                fits = fits && t.size(i) == *want;
+                ++i;
+            }
+            *p = t.data_ptr();
+        }))
+        return false;
+    return fits || wrong(what);
+}
+
+struct Adapters {
+    void *a, *b, *offsets, *ids, *scale;
+    int w_type;
+    int64_t G = -1, R = -1, S = -1;
+};
+
+bool adapters(PyObject* oa, PyObject* ob, PyObject* ooffsets, PyObject* oids, PyObject* oscale, int64_t K, int64_t N, Adapters* w)
+{
+    at::ScalarType type = at::kFloat;
+    if (!THPVariable_Check(oa))
+        return wrong("a: expected a tensor");
+    if (!guarded([&] { type = THPVariable_Unpack(oa).scalar_type(); }))
+        return false;
+    w->w_type = real_type(type);
+    if (w->w_type < 0)
+        return wrong("a: expected float32, bfloat16 or float16");
+    int64_t ends;
+    if (!array(oa, false, type, {&w->G, &w->R, &K}, &w->a, "a: expected a contiguous tensor [G][R][K] on the current device") ||
+        !array(ob, false, type, {&w->G, &N, &w->R}, &w->b, "b: expected a contiguous tensor [G][N][R] of a's type on the current device") ||
+        !array(oids, false, at::kInt, {&w->S}, &w->ids, "ids: expected int32 [S] on the current device"))
+        return false;
+    ends = w->S + 1;
+    return array(ooffsets, false, at::kInt, {&ends}, &w->offsets, "offsets: expected int32 [S + 1] on the current device") &&
+           array(oscale, true, at::kFloat, {&w->G}, &w->scale, "scale: expected float32 [G] on the current device");
+}
+
+bool like(const Matrix& m, const Matrix& of, int64_t cols) { return !m.p || (m.type == of.type && m.rows == of.rows && m.cols == cols); }
+
+int count32(int64_t v) { return v > 0x7fffffff ? 0x7fffffff : (int)v; }     // (what does not fit is refused by the library)
+
+// adapter_forward(x, a, b, offsets, ids, scale, base, y, u) -> status
+PyObject* adapter_forward(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    Matrix x, base, y;
+    Adapters w;
+    void *u, *st;
+    if (!arguments(n, 9) || !matrix(a[0], false, &x, "x: expected [M][K] of float32, bfloat16 or float16, columns side by side, on the current device") ||
+        !matrix(a[7], false, &y, "y: expected [M][N] of x's type, columns side by side, on the current device") ||
+        !matrix(a[6], true, &base, "base: expected [M][N] of x's type, columns side by side, on the current device") ||
+        !adapters(a[1], a[2], a[3], a[4], a[5], x.cols, y.cols, &w))
+        return nullptr;
+    if (y.type != x.type || y.rows != x.rows || !like(base, x, y.cols)) {
+        wrong("expected y and base [M][N] of x's type");
+        return nullptr;
+    }
+    if (!array(a[8], true, at::kFloat, {&x.rows, &w.R}, &u, "u: expected contiguous float32 [M][R] on the current device") || !stream(&st))
+        return nullptr;
+    fpq_status status;
+    Py_BEGIN_ALLOW_THREADS
+    status = fpq_adapter_forward(x.p, x.ld, x.type, w.a, w.b, w.w_type, (const float*)w.scale, count32(w.G), count32(w.R),
+                                 (const int32_t*)w.offsets, (const int32_t*)w.ids, count32(w.S), base.p, base.ld, y.p, y.ld, (float*)u,
+                                 x.rows, y.cols, x.cols, st);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(status);
+}
+
+// adapter_backward(dy, x, u, a, b, offsets, ids, scale, base, dx, da, db, workspace) -> status
+PyObject* adapter_backward(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    Matrix dy, x, base, dx;
+    Adapters w;
+    void *u, *da, *db, *work, *st;
+    size_t work_bytes;
+    if (!arguments(n, 13) || !matrix(a[0], false, &dy, "dy: expected [M][N] of float32, bfloat16 or float16, columns side by side, on the current device") ||
+        !matrix(a[1], false, &x, "x: expected [M][K] of dy's type, columns side by side, on the current device") ||
+        !matrix(a[8], true, &base, "base: expected [M][K] of dy's type, columns side by side, on the current device") ||
+        !matrix(a[9], true, &dx, "dx: expected [M][K] of dy's type, columns side by side, on the current device") ||
+        !adapters(a[3], a[4], a[5], a[6], a[7], x.cols, dy.cols, &w))
+        return nullptr;
+    if (dy.type != x.type || dy.rows != x.rows || !like(base, x, x.cols) || !like(dx, x, x.cols)) {
+        wrong("expected dy [M][N] and x, base, dx [M][K] of one type");
+        return nullptr;
+    }
+    if (!array(a[2], false, at::kFloat, {&x.rows, &w.R}, &u, "u: expected contiguous float32 [M][R] on the current device") ||
+        !array(a[10], false, at::kFloat, {&w.G, &w.R, &x.cols}, &da, "da: expected contiguous float32 [G][R][K] on the current device") ||
+        !array(a[11], false, at::kFloat, {&w.G, &dy.cols, &w.R}, &db, "db: expected contiguous float32 [G][N][R] on the current device") ||
+        !workspace(a[12], &work, &work_bytes) || !stream(&st))
+        return nullptr;
+    fpq_status status;
+    Py_BEGIN_ALLOW_THREADS
+    status = fpq_adapter_backward(dy.p, dy.ld, x.p, x.ld, x.type, (const float*)u, w.a, w.b, w.w_type, (const float*)w.scale, count32(w.G),
+                                  count32(w.R), (const int32_t*)w.offsets, (const int32_t*)w.ids, count32(w.S), base.p, base.ld, dx.p,
+                                  dx.ld, (float*)da, (float*)db, x.rows, dy.cols, x.cols, work, work_bytes, st);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(status);
+}
+
+// adamw_step(descriptors, device, g_type, copy_type, state_type, lr, beta1, beta2, eps, weight_decay, seed, factors, step) -> status
+// (descriptors: the bytes of an array of fpq_adamw_tensor whose tensors lie on `device`)
+PyObject* adamw_step(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    int device, type[3];
+    double o[5];
+    void *factors, *step, *st;
+    int64_t seed, two = 2;
+    if (!arguments(n, 13) || !integer(a[1], &device) || !integer(a[2], &type[0]) || !integer(a[3], &type[1]) || !integer(a[4], &type[2]))
+        return nullptr;
+    for (int i = 0; i < 5; ++i) {
+        o[i] = PyFloat_AsDouble(a[5 + i]);
+        if (o[i] == -1.0 && PyErr_Occurred())
+            return nullptr;
+    }
+    bool here = false;
+    if (!integer(a[10], &seed) || !guarded([&] { here = c10::cuda::current_device() == device; }))
+        return nullptr;
+    if (!here) {
+        wrong("the tensors lie on another device than the current one");
+        return nullptr;
+    }
+    if (seed < 0 || seed > 0xffffffffll) {
+        PyErr_SetString(PyExc_ValueError, "seed: expected 32 bits");
+        return nullptr;
+    }
+    if (!array(a[11], true, at::kFloat, {&two}, &factors, "factors: expected float32 [2] on the current device") ||
+        !array(a[12], false, at::kLong, {&two}, &step, "step: expected int64 [2] on the current device") || !stream(&st))
+        return nullptr;
+    Py_buffer view;
+    if (PyObject_GetBuffer(a[0], &view, PyBUF_SIMPLE) != 0)
+        return nullptr;
+    const fpq_adamw_options options = {o[0], o[1], o[2], o[3], o[4], (uint32_t)seed, 0};
+    fpq_status status;
+    Py_BEGIN_ALLOW_THREADS
+    status = fpq_adamw_step((const fpq_adamw_tensor*)view.buf, count32(view.len / (Py_ssize_t)sizeof(fpq_adamw_tensor)), type[0], type[1], type[2],
+                            &options, (const float*)factors, (int64_t*)step, st);
+    Py_END_ALLOW_THREADS
+    PyBuffer_Release(&view);
+    return PyLong_FromLong(status);
+}
+
 PyMethodDef methods[] = {
     {"linear", (PyCFunction)(void (*)(void))linear, METH_FASTCALL, nullptr},
     {"conv2d", (PyCFunction)(void (*)(void))conv2d, METH_FASTCALL, nullptr},
     {"conv2d_split", (PyCFunction)(void (*)(void))conv2d_split, METH_FASTCALL, nullptr},
     {"search", (PyCFunction)(void (*)(void))search, METH_FASTCALL, nullptr},
     {"learn_step", (PyCFunction)(void (*)(void))learn_step, METH_FASTCALL, nullptr},
+    {"adapter_forward", (PyCFunction)(void (*)(void))adapter_forward, METH_FASTCALL, nullptr},
+    {"adapter_backward", (PyCFunction)(void (*)(void))adapter_backward, METH_FASTCALL, nullptr},
+    {"adamw_step", (PyCFunction)(void (*)(void))adamw_step, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 

@@ -1,0 +1,398 @@
+"""Low-rank adapters of many requests: forward and backward against the formulas in 64 bits."""
+import ctypes
+
+import pytest
+import torch
+
+import paper_2408_06995_b200 as fpq
+from paper_2408_06995_b200 import build as fpq_build
+
+fpq_build.build()
+F32, BF, HF = torch.float32, torch.bfloat16, torch.float16
+
+
+# ---- refusals, without a GPU ------------------------------------------------------------------------------------------
+
+class Call:
+    """fpq_adapter_forward / _backward with arguments that pass, but for those that a test changes; nothing is ever launched."""
+    forward = ["x", "ldx", "x_type", "a", "b", "w_type", "scale", "G", "R", "offsets", "ids", "S", "base", "ld_base", "y", "ldy", "u", "M", "N",
+               "K", "stream"]
+    backward = ["dy", "ld_dy", "x", "ldx", "x_type", "u", "a", "b", "w_type", "scale", "G", "R", "offsets", "ids", "S", "base", "ld_base", "dx",
+                "ld_dx", "da", "db", "M", "N", "K", "workspace", "ws_bytes", "stream"]
+
+    def __init__(self, **given):
+        pointers = {k: 4096 for k in ("x", "a", "b", "scale", "offsets", "ids", "base", "y", "u", "dy", "dx", "da", "db", "workspace")}
+        self.v = {**pointers, "x_type": fpq.FP32, "w_type": fpq.FP32, "G": 2, "R": 4, "S": 3, "M": 10, "N": 8, "K": 16, "ldx": 16, "ldy": 8,
+                  "ld_base": 8, "ld_dy": 8, "ld_dx": 16, "ws_bytes": 10 * 4 * 4 + 16, "stream": None, **given}
+
+    def run(self, name):
+        return getattr(fpq.lib(), "fpq_adapter_" + name)(*[self.v[k] for k in getattr(self, name)])
+
+
+BAD = [({"x_type": 3}, "ERR_UNSUPPORTED"), ({"x_type": -1}, "ERR_UNSUPPORTED"), ({"w_type": 3}, "ERR_UNSUPPORTED"),
+       ({"x_type": fpq.BF16}, "ERR_UNSUPPORTED"), ({"x_type": fpq.FP16, "w_type": fpq.BF16}, "ERR_UNSUPPORTED"),
+       ({"M": -1}, "ERR_SHAPE"), ({"M": 1 << 31}, "ERR_SHAPE"), ({"N": 0}, "ERR_SHAPE"), ({"K": 0}, "ERR_SHAPE"), ({"K": (1 << 24) + 1}, "ERR_SHAPE"),
+       ({"G": 0}, "ERR_SHAPE"), ({"G": 65536}, "ERR_SHAPE"), ({"R": 0}, "ERR_SHAPE"), ({"R": 129}, "ERR_SHAPE"), ({"S": -1}, "ERR_SHAPE"),
+       ({"S": (1 << 24) + 1}, "ERR_SHAPE"), ({"ldx": 15}, "ERR_SHAPE"), ({"G": 65535, "R": 128, "N": 1 << 18}, "ERR_SHAPE"),
+       ({"a": None}, "ERR_NULL"), ({"b": None}, "ERR_NULL"), ({"offsets": None}, "ERR_NULL"), ({"ids": None}, "ERR_NULL"), ({"x": None}, "ERR_NULL"),
+       ({"x": 4098}, "ERR_ALIGN"), ({"a": 4098}, "ERR_ALIGN"), ({"b": 4097}, "ERR_ALIGN"), ({"scale": 4098}, "ERR_ALIGN"),
+       ({"offsets": 4098}, "ERR_ALIGN"), ({"ids": 4097}, "ERR_ALIGN"), ({"base": 4098}, "ERR_ALIGN"), ({"u": 4098}, "ERR_ALIGN")]
+
+
+@pytest.mark.parametrize("given,error", BAD + [({"y": None}, "ERR_NULL"), ({"y": 4097}, "ERR_ALIGN"), ({"ldy": 7}, "ERR_SHAPE"),
+                                               ({"ld_base": 7}, "ERR_SHAPE")])
+def test_forward_refuses(given, error):
+    assert Call(**given).run("forward") == getattr(fpq, error)
+
+
+@pytest.mark.parametrize("given,error", BAD + [({"u": None}, "ERR_NULL"), ({"dy": None}, "ERR_NULL"), ({"da": None}, "ERR_NULL"),
+                                               ({"db": None}, "ERR_NULL"), ({"dy": 4098}, "ERR_ALIGN"), ({"da": 4098}, "ERR_ALIGN"),
+                                               ({"dx": 4098}, "ERR_ALIGN"), ({"workspace": 4100}, "ERR_ALIGN"), ({"ld_dy": 7}, "ERR_SHAPE"),
+                                               ({"ld_dx": 15}, "ERR_SHAPE"), ({"ld_base": 15}, "ERR_SHAPE"), ({"workspace": None}, "ERR_WORKSPACE"),
+                                               ({"ws_bytes": 10 * 4 * 4 + 15}, "ERR_WORKSPACE")])
+def test_backward_refuses(given, error):
+    assert Call(**{"ld_base": 16, "N": 8, **({"ld_dy": given["N"]} if "N" in given and given["N"] > 8 else {}), **given}).run("backward") == getattr(fpq, error)
+
+
+def test_nothing_to_do_is_no_error():
+    assert Call(M=0, x=None, y=None).run("forward") == fpq.OK
+    assert Call(S=0, ids=None).run("forward") == fpq.OK
+
+
+def test_workspace_size():
+    assert fpq.fpq_adapter_backward_workspace_size(1000, 16) >= 1000 * 16 * 4
+    assert fpq.fpq_adapter_backward_workspace_size(-1, 16) == 0 and fpq.fpq_adapter_backward_workspace_size(10, 129) == 0
+
+
+def test_binding_takes_no_cpu_tensors():
+    x, a, b = torch.zeros(4, 8), torch.zeros(1, 2, 8), torch.zeros(1, 8, 2)
+    i = torch.zeros(2, dtype=torch.int32)
+    with pytest.raises(AssertionError, match="current device"):
+        fpq.fpq_adapter_forward(x, a, b, i, i[:1])
+    with pytest.raises(TypeError):
+        fpq._load_layers().adapter_forward(x)
+
+
+# ---- on the GPU -------------------------------------------------------------------------------------------------------
+
+def make(M, K, N, R, cuts, ids, G, xt=F32, wt=F32, seed=0, ldx=None, ldy=None, scale=True):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+
+    def normal(*shape):
+        return torch.randn(*shape, generator=g, device="cuda")
+
+    ldx, ldy = ldx or K, ldy or N
+    return {"x": normal(M, ldx).to(xt)[:, :K], "a": (normal(G, R, K) / K ** 0.5).to(wt), "b": (normal(G, N, R) * 0.3).to(wt),
+            "scale": torch.rand(G, generator=g, device="cuda") + 0.5 if scale else None,
+            "offsets": torch.tensor(cuts, dtype=torch.int32, device="cuda"), "ids": torch.tensor(ids, dtype=torch.int32, device="cuda"),
+            "base": normal(M, ldy).to(xt)[:, :N], "dy": normal(M, ldy).to(xt)[:, :N], "dbase": normal(M, ldx).to(xt)[:, :K]}
+
+
+def segments(t):
+    cuts, ids, G = t["offsets"].tolist(), t["ids"].tolist(), t["a"].shape[0]
+    return [(lo, hi, i if 0 <= i < G else -1) for lo, hi, i in zip(cuts, cuts[1:], ids) if hi > lo]
+
+
+def product_error(D, terms):
+    """Error of a sum of D products relative to the sum of their magnitudes: two TF32 terms each (2^-22 left out, 2^-23 of each second term
+    cut off), at most `terms` cut-off additions of the tensor cores, each 2^-23 at most, and the FP32 additions behind them."""
+    return 2.0 ** -21 + (terms + 20 + D / 64) * 2.0 ** -23
+
+
+def half_step(t, v):
+    tiny = {F32: 2.0 ** -149, BF: 2.0 ** -133, HF: 2.0 ** -24}[t]
+    return torch.finfo(t).eps / 2 * v.abs() + tiny / 2
+
+
+def rows_exact(x, w1, w2, base, s, R):
+    """t, y and their error bounds for the rows of one adapter: t = x w1^T, y = base + s t w2^T."""
+    D1 = x.shape[1]
+    t = x @ w1.T
+    dt = product_error(D1, 24) * (x.abs() @ w1.abs().T)
+    y = s * (t @ w2.T)
+    dy = s * (dt @ w2.abs().T + (product_error(R, 3 * R / 8) + 2.0 ** -23) * (t.abs() @ w2.abs().T))
+    if base is not None:
+        y = y + base
+    return t, dt, y, dy + 2.0 ** -23 * y.abs()
+
+
+def check_rows(got, y, dy, what):
+    err = (got.double() - y).abs()
+    tol = dy + half_step(got.dtype, y.abs() + dy)
+    worst = (err - tol).argmax()
+    assert bool((err <= tol).all()), (what, float(err.flatten()[worst]), float(tol.flatten()[worst]))
+
+
+def run_forward(t, base=True, in_place=False, ldy=None):
+    M, N, R = t["x"].shape[0], t["b"].shape[1], t["a"].shape[1]
+    y = torch.full((M, ldy or N), -7.0, dtype=t["x"].dtype, device="cuda")[:, :N]
+    u = torch.full((M, R), -7.0, device="cuda")
+    if in_place:
+        y.copy_(t["base"])
+    before = y.clone()
+    fpq.fpq_adapter_forward(t["x"], t["a"], t["b"], t["offsets"], t["ids"], t["scale"], y if in_place else t["base"] if base else None, y, u)
+    return before, y, u
+
+
+def check_forward(t, before, y, u, base=True):
+    inside = torch.zeros(y.shape[0], dtype=torch.bool, device="cuda")
+    for lo, hi, i in segments(t):
+        inside[lo:hi] = True
+        b0 = t["base"][lo:hi].double() if base else None
+        if i < 0:
+            assert torch.equal(y[lo:hi], t["base"][lo:hi] if base else torch.zeros_like(y[lo:hi])) and not bool(u[lo:hi].any())
+            continue
+        s = float(t["scale"][i]) if t["scale"] is not None else 1.0
+        te, dt, ye, dy = rows_exact(t["x"][lo:hi].double(), t["a"][i].double(), t["b"][i].double(), b0, s, u.shape[1])
+        check_rows(u[lo:hi], te, dt, "u")
+        check_rows(y[lo:hi], ye, dy, "y")
+    assert torch.equal(y[~inside], before[~inside]) and bool((u[~inside] == -7).all())
+
+
+SHAPES = [  # M, K, N, R, cuts, ids, G
+    (1, 1280, 1280, 16, [0, 1], [0], 1),
+    (1, 1, 1, 1, [0, 1], [0], 1),
+    (5, 320, 320, 8, [0, 1, 2, 3, 4, 5], [4, 0, -1, 2, 0], 5),
+    (64, 640, 320, 16, list(range(65)), [i % 7 for i in range(64)], 7),
+    (77, 768, 320, 4, [0, 77], [0], 1),
+    (130, 35, 33, 3, [0, 17, 17, 64, 130], [1, 0, 2, 1], 3),
+    (200, 802, 70, 24, [3, 40, 171], [1, 0], 2),
+    (333, 96, 257, 17, [0, 100, 300], [9, 0], 1),
+    (256, 320, 640, 32, [0, 33, 256], [0, 1], 2),
+    (150, 200, 132, 64, [0, 64, 150], [1, 0], 2),
+    (100, 136, 72, 128, [0, 31, 100], [0, 1], 2),
+    (90, 64, 40, 100, [0, 90], [0], 1),
+    (4100, 320, 96, 16, [0, 4096, 4099], [0, 0], 1),
+    (40, 4100, 36, 40, [0, 40], [0], 1),
+]
+TYPES = [(F32, F32), (F32, BF), (F32, HF), (BF, BF), (HF, HF)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("xt,wt", TYPES)
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s[:4])))
+def test_forward(shape, xt, wt):
+    t = make(*shape, xt=xt, wt=wt)
+    check_forward(t, *run_forward(t))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("xt,wt", TYPES)
+@pytest.mark.parametrize("ldx,ldy", [(700, 1000), (643, 963)])
+def test_forward_in_slices_of_wider_tensors(xt, wt, ldx, ldy):
+    t = make(100, 640, 960, 16, [0, 60, 100], [1, 0], 2, xt, wt, ldx=ldx, ldy=ldy)
+    check_forward(t, *run_forward(t, ldy=ldy))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("xt", [F32, BF])
+def test_forward_base_absent_or_in_place(xt):
+    t = make(300, 320, 96, 16, [0, 100, 120, 290], [1, -1, 0], 2, xt, xt, scale=False)
+    check_forward(t, *run_forward(t, base=False), base=False)
+    before, y, u = run_forward(t, in_place=True)
+    check_forward(t, before, y, u)
+    assert torch.equal(y, fpq.fpq_adapter_forward(t["x"], t["a"], t["b"], t["offsets"], t["ids"], None, t["base"]))
+
+
+@pytest.mark.gpu
+def test_rows_of_no_segment_are_not_read():
+    t = make(64, 320, 64, 16, [8, 20, 50], [0, 1], 2)
+    clean = run_forward(t)[1].clone()
+    t["x"][:8], t["x"][50:], t["base"][50:] = float("nan"), float("inf"), float("nan")
+    y = run_forward(t)[1]
+    assert torch.equal(y, clean)
+    t["dy"][:8] = float("nan")
+    u = torch.randn(64, 16, device="cuda")
+    u[:8], u[50:] = float("nan"), float("inf")
+    for g in fpq.fpq_adapter_backward(t["dy"], t["x"], u, t["a"], t["b"], t["offsets"], t["ids"], t["scale"])[1:]:
+        assert bool(torch.isfinite(g).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan"), 3.4e38])
+def test_forward_values_without_a_split(value):
+    """One operand that is not finite (or rounds up to infinity as TF32): what multiply-adds give, and no other row changes."""
+    t = make(40, 256, 48, 8, [0, 40], [0], 1)
+    clean, cu = (v.clone() for v in run_forward(t)[1:])
+    t["x"][5, 77] = value
+    _, y, u = run_forward(t)
+    others = torch.arange(40, device="cuda") != 5
+    assert torch.equal(y[others], clean[others]) and torch.equal(u[others], cu[others])
+    want = t["x"][5].float().cpu() @ t["a"][0].cpu().T
+    got = u[5].cpu()
+    assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(torch.isinf(got), torch.isinf(want))
+    fine = torch.isfinite(want)
+    assert torch.equal(got[~fine & ~torch.isnan(want)], want[~fine & ~torch.isnan(want)])
+    bound = product_error(256, 24) * (t["x"][5].cpu().double().abs() @ t["a"][0].cpu().double().abs().T)
+    assert bool(((got.double() - t["x"][5].cpu().double() @ t["a"][0].cpu().double().T).abs()[fine] <= bound[fine]).all())
+
+
+@pytest.mark.gpu
+def test_wrong_lists_stay_in_bounds():
+    """Offsets out of range are clamped and ids out of range mean no adapter: every row keeps base or gets some adapter's result."""
+    t = make(50, 64, 32, 8, [-100, 20, 1000], [0, 5], 2)
+    _, y, _ = run_forward(t)
+    assert torch.equal(y[20:], t["base"][20:])
+    _, _, want, dy = rows_exact(t["x"][:20].double(), t["a"][0].double(), t["b"][0].double(), t["base"][:20].double(), float(t["scale"][0]), 8)
+    check_rows(y[:20], want, dy, "y")
+    t["offsets"] = torch.tensor([40, 10, 45], dtype=torch.int32, device="cuda")
+    run_forward(t)
+    torch.cuda.synchronize()
+
+
+@pytest.mark.gpu
+def test_replayed_with_other_segments():
+    t = make(120, 320, 64, 16, [0, 50, 120], [0, 1], 3)
+    y, u = torch.zeros(120, 64, device="cuda"), torch.zeros(120, 16, device="cuda")
+    da, db, dx = torch.zeros_like(t["a"]), torch.zeros_like(t["b"]), torch.zeros(120, 320, device="cuda")
+    ws = torch.empty(fpq.fpq_adapter_backward_workspace_size(120, 16), dtype=torch.uint8, device="cuda")
+
+    def both():
+        fpq.fpq_adapter_forward(t["x"], t["a"], t["b"], t["offsets"], t["ids"], t["scale"], t["base"], y, u)
+        fpq.fpq_adapter_backward(t["dy"], t["x"], u, t["a"], t["b"], t["offsets"], t["ids"], t["scale"], None, dx, da, db, ws)
+
+    both()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both()
+    t["offsets"].copy_(torch.tensor([0, 9, 113], dtype=torch.int32))
+    t["ids"].copy_(torch.tensor([2, 0], dtype=torch.int32))
+    for v in (y, u, dx, da, db):
+        v.fill_(-7.0)
+    graph.replay()
+    got = [v.clone() for v in (y, u, dx, da, db)]
+    for v in (y, u, dx, da, db):
+        v.fill_(-7.0)
+    both()
+    for v, w in zip(got, (y, u, dx, da, db)):
+        assert torch.equal(v, w)
+    check_forward(t, torch.full_like(y, -7.0), y, u)
+
+
+def check_backward(t, u, dx, da, db, before, base=True, have_dx=True):
+    R, G = u.shape[1], t["a"].shape[0]
+    ea, eb = torch.zeros_like(t["a"], dtype=torch.float64), torch.zeros_like(t["b"], dtype=torch.float64)
+    ta, tb = torch.zeros_like(ea), torch.zeros_like(eb)
+    inside = torch.zeros(u.shape[0], dtype=torch.bool, device="cuda")
+    M = u.shape[0]
+    for lo, hi, i in segments(t):
+        inside[lo:hi] = True
+        b0 = t["dbase"][lo:hi].double() if base else None
+        if i < 0:
+            if have_dx:
+                assert torch.equal(dx[lo:hi], t["dbase"][lo:hi] if base else torch.zeros_like(dx[lo:hi]))
+            continue
+        s = float(t["scale"][i]) if t["scale"] is not None else 1.0
+        dy, x, uu = t["dy"][lo:hi].double(), t["x"][lo:hi].double(), u[lo:hi].double()
+        te, dt, xe, dxe = rows_exact(dy, t["b"][i].double().T, t["a"][i].double().T, b0, s, R)
+        if have_dx:
+            check_rows(dx[lo:hi], xe, dxe, "dx")
+        te, dt = s * te, s * dt + 2.0 ** -23 * s * te.abs()
+        ea[i] += te.T @ x
+        ta[i] += dt.T @ x.abs() + product_error(M, 24) * (te.abs().T @ x.abs())
+        eb[i] += s * (dy.T @ uu)
+        tb[i] += s * (product_error(M, 24) + 2.0 ** -23) * (dy.abs().T @ uu.abs())
+    check_rows(da, ea, ta, "da")
+    check_rows(db, eb, tb, "db")
+    if have_dx:
+        assert torch.equal(dx[~inside], before[~inside])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("xt,wt", TYPES)
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s[:4])))
+def test_backward(shape, xt, wt):
+    t = make(*shape, xt=xt, wt=wt)
+    M, K, R = t["x"].shape[0], t["x"].shape[1], t["a"].shape[1]
+    u = torch.randn(M, R, device="cuda")
+    dx = torch.full((M, K), -7.0, dtype=xt, device="cuda")
+    before = dx.clone()
+    _, da, db = fpq.fpq_adapter_backward(t["dy"], t["x"], u, t["a"], t["b"], t["offsets"], t["ids"], t["scale"], t["dbase"], dx)
+    check_backward(t, u, dx, da, db, before)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("xt", [F32, HF])
+def test_backward_strides_in_place_and_without_dx(xt):
+    t = make(210, 640, 320, 16, [0, 90, 100, 205], [1, -1, 0], 3, xt, xt, ldx=643, ldy=328)
+    u = torch.randn(210, 16, device="cuda")
+    args = (t["dy"], t["x"], u, t["a"], t["b"], t["offsets"], t["ids"], t["scale"])
+    none, da, db = fpq.fpq_adapter_backward(*args, need_dx=False)
+    assert none is None
+    check_backward(t, u, None, da, db, None, have_dx=False)
+    dx = t["dbase"].clone()
+    before = dx.clone()
+    _, da2, db2 = fpq.fpq_adapter_backward(*args, base=dx, dx=dx)
+    check_backward(t, u, dx, da2, db2, before)
+    assert torch.equal(da, da2) and torch.equal(db, db2)
+    assert not bool(da2[2].any()) and not bool(db2[2].any())          # an adapter without rows
+
+
+@pytest.mark.gpu
+def test_backward_without_rows_gives_zeros():
+    for M, cuts, ids in ((0, [0, 0], [0]), (4, [0], [])):
+        t = make(M, 40, 24, 4, cuts, ids, 2)
+        _, da, db = fpq.fpq_adapter_backward(t["dy"], t["x"], torch.zeros(M, 4, device="cuda"), t["a"], t["b"], t["offsets"], t["ids"])
+        assert not bool(da.any()) and not bool(db.any())
+
+
+@pytest.mark.gpu
+def test_gradients_against_differences():
+    """y is linear in each of x, A and B alone: <dy, y(A + d) - y(A)> is <dA, d> but for rounding (64-bit sums of FP32 results)."""
+    t = make(150, 96, 80, 8, [0, 70, 150], [1, 0], 2)
+
+    def forward(**changed):
+        c = {**t, **changed}
+        y, u = torch.zeros(150, 80, device="cuda"), torch.zeros(150, 8, device="cuda")
+        fpq.fpq_adapter_forward(c["x"], c["a"], c["b"], c["offsets"], c["ids"], c["scale"], None, y, u)
+        return y.double(), u
+
+    y0, u = forward()
+    dy = t["dy"].double()
+    dx, da, db = fpq.fpq_adapter_backward(t["dy"], t["x"], u, t["a"], t["b"], t["offsets"], t["ids"], t["scale"])
+    for name, grad in (("x", dx), ("a", da), ("b", db)):
+        d = torch.randn_like(t[name])
+        moved = (t[name] + d)                                          # (rounded: the step that was made is moved - t[name])
+        y1, _ = forward(**{name: moved})
+        lhs = float((dy * (y1 - y0)).sum())
+        rhs = float((grad.double() * (moved.double() - t[name].double())).sum())
+        # each y is off by less than 2^-16 of its magnitude (product_error of 96 and 8 terms, twice the sum of magnitudes)
+        size = float((dy.abs() * (y1.abs() + y0.abs())).sum()) + float((grad.double().abs() * d.double().abs()).sum())
+        assert abs(lhs - rhs) <= 2.0 ** -15 * size, (name, lhs, rhs)
+
+
+@pytest.mark.gpu
+def test_equal_calls_give_equal_bits_on_two_streams():
+    t = make(2000, 640, 320, 16, [0, 700, 2000], [1, 0], 2)
+    u = torch.randn(2000, 16, device="cuda")
+    args = (t["dy"], t["x"], u, t["a"], t["b"], t["offsets"], t["ids"], t["scale"])
+    want = fpq.fpq_adapter_backward(*args)
+    torch.cuda.synchronize()
+    got, streams = [], [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(4):
+        for s in streams:
+            with torch.cuda.stream(s):
+                got.append(fpq.fpq_adapter_backward(*args))
+    torch.cuda.synchronize()
+    for g in got:
+        assert all(torch.equal(a, b) for a, b in zip(g, want))
+
+
+@pytest.mark.gpu
+def test_binding_refuses():
+    t = make(10, 32, 16, 4, [0, 10], [0], 1)
+    ok = [t["x"], t["a"], t["b"], t["offsets"], t["ids"], t["scale"], t["base"], torch.zeros(10, 16, device="cuda"), None]
+    for at, bad in ((0, t["x"].double()), (0, t["x"].T), (0, t["x"][:, :31]), (0, t["x"][:1].expand(10, 32)), (1, t["a"].half()), (1, t["a"][0]),
+                    (2, t["b"][:, :15]), (3, t["offsets"].long()), (3, t["offsets"][:1]), (4, t["ids"].cpu()), (5, t["scale"].half()),
+                    (6, t["base"][:9]), (6, t["base"].bfloat16()), (7, torch.zeros(9, 16, device="cuda")), (8, torch.zeros(10, 5, device="cuda"))):
+        with pytest.raises(AssertionError):
+            fpq.fpq_adapter_forward(*(bad if i == at else v for i, v in enumerate(ok)))
+    big = torch.zeros(1, 129, 32, device="cuda"), torch.zeros(1, 16, 129, device="cuda")
+    with pytest.raises(fpq.FpqError, match="shape"):
+        fpq.fpq_adapter_forward(t["x"], *big, *ok[3:])
+    with pytest.raises(fpq.FpqError, match="unsupported"):
+        fpq.fpq_adapter_forward(t["x"].half(), t["a"], t["b"], t["offsets"], t["ids"])
+
+
+def test_ctypes_signature_matches_the_header():
+    assert ctypes.sizeof(fpq._CAdamwTensor) == 64
