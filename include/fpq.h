@@ -445,8 +445,8 @@ fpq_status fpq_round_learn_harden(const float* alpha, int64_t N, int64_t K, uint
  *   dx       [M][K] out, or NULL when x needs no gradient; rows in no segment stay as they were
  *   da, db   [G][R][K] and [G][N][R] FP32 out, overwritten (zeros for an adapter without rows).  No atomics: equal calls
  *            give equal bits
- *   workspace  fpq_adapter_backward_workspace_size(M, R) bytes, 16-byte aligned, contents not kept
- * One kernel forward, two backward, on `stream`; no allocation, no synchronisation.  Pointers are aligned to their
+ *   workspace  fpq_adapter_backward_workspace_size bytes (0 for sizes out of range), 16-byte aligned, contents not kept
+ * One kernel forward, three backward, on `stream`; no allocation, no synchronisation.  Pointers are aligned to their
  * element; rows at multiples of 16 bytes are read 16 bytes at a time.  Limits: M and S below 2^31 and 2^24, N and K
  * up to 2^24, G up to 65535, G * R * max(N, K) below 2^40.  M = 0 or S = 0: forward does nothing, backward writes zeros to
  * da and db.  Errors: FPQ_ERR_UNSUPPORTED, FPQ_ERR_SHAPE, FPQ_ERR_NULL, FPQ_ERR_ALIGN, FPQ_ERR_WORKSPACE, FPQ_ERR_CUDA.
@@ -456,7 +456,7 @@ fpq_status fpq_adapter_forward(const void* x, int64_t ldx, int32_t x_type, const
                                const float* scale, int32_t G, int32_t R, const int32_t* offsets, const int32_t* ids, int32_t S,
                                const void* base, int64_t ld_base, void* y, int64_t ldy, float* u, int64_t M, int64_t N, int64_t K,
                                void* stream);
-size_t fpq_adapter_backward_workspace_size(int64_t M, int32_t R);
+size_t fpq_adapter_backward_workspace_size(int64_t M, int64_t N, int64_t K, int32_t G, int32_t R, int32_t w_type);
 fpq_status fpq_adapter_backward(const void* dy, int64_t ld_dy, const void* x, int64_t ldx, int32_t x_type, const float* u,
                                 const void* a, const void* b, int32_t w_type, const float* scale, int32_t G, int32_t R,
                                 const int32_t* offsets, const int32_t* ids, int32_t S, const void* base, int64_t ld_base, void* dx,

@@ -172,7 +172,7 @@ def lib() -> ctypes.CDLL:
         L.fpq_adapter_forward.restype = i32
         L.fpq_adapter_forward.argtypes = [vp, i64, i32, vp, vp, i32, vp, i32, i32, vp, vp, i32, vp, i64, vp, i64, vp, i64, i64, i64, vp]
         L.fpq_adapter_backward_workspace_size.restype = sz
-        L.fpq_adapter_backward_workspace_size.argtypes = [i64, i32]
+        L.fpq_adapter_backward_workspace_size.argtypes = [i64, i64, i64, i32, i32, i32]
         L.fpq_adapter_backward.restype = i32
         L.fpq_adapter_backward.argtypes = [vp, i64, vp, i64, i32, vp, vp, vp, i32, vp, i32, i32, vp, vp, i32, vp, i64, vp, i64, vp, vp,
                                            i64, i64, i64, vp, sz, vp]
@@ -480,6 +480,9 @@ def fpq_round_learn_harden(alpha: torch.Tensor, bits: torch.Tensor = None) -> to
     return bits
 
 
+_REAL = {torch.float32: FP32, torch.bfloat16: BF16, torch.float16: FP16}
+
+
 def fpq_adapter_forward(x: torch.Tensor, a: torch.Tensor, b: torch.Tensor, offsets: torch.Tensor, ids: torch.Tensor, scale=None, base=None,
                         y: torch.Tensor = None, u: torch.Tensor = None) -> torch.Tensor:
     """y[i] = base[i] + scale[g] B[g] (A[g] x[i]) for the rows i of segment s, g = ids[s].  x [M][K], base and y [M][N] of float32,
@@ -494,8 +497,8 @@ def fpq_adapter_forward(x: torch.Tensor, a: torch.Tensor, b: torch.Tensor, offse
     return y
 
 
-def fpq_adapter_backward_workspace_size(M: int, R: int) -> int:
-    return lib().fpq_adapter_backward_workspace_size(int(M), int(R))
+def fpq_adapter_backward_workspace_size(M: int, N: int, K: int, G: int, R: int, w_type: int) -> int:
+    return lib().fpq_adapter_backward_workspace_size(int(M), int(N), int(K), int(G), int(R), int(w_type))
 
 
 def fpq_adapter_backward(dy: torch.Tensor, x: torch.Tensor, u: torch.Tensor, a: torch.Tensor, b: torch.Tensor, offsets: torch.Tensor,
@@ -512,7 +515,8 @@ def fpq_adapter_backward(dy: torch.Tensor, x: torch.Tensor, u: torch.Tensor, a: 
     if db is None:
         db = torch.empty(b.shape, dtype=torch.float32, device=b.device)
     if workspace is None:
-        workspace = torch.empty(max(16, fpq_adapter_backward_workspace_size(x.shape[0], a.shape[1])), dtype=torch.uint8, device=x.device)
+        size = fpq_adapter_backward_workspace_size(x.shape[0], b.shape[1], x.shape[1], *a.shape[:2], _REAL.get(a.dtype, -1))
+        workspace = torch.empty(max(16, size), dtype=torch.uint8, device=x.device)
     code = (_layers or _load_layers()).adapter_backward(dy, x, u, a, b, offsets, ids, scale, base, dx, da, db, workspace)
     if code:
         raise FpqError(code, "fpq_adapter_backward")
@@ -529,17 +533,16 @@ class AdamwTable:
 
     def __init__(self, params, grads, m, v, m_scale=None, v_scale=None, copies=None):
         count = len(params)
-        real = {torch.float32: FP32, torch.bfloat16: BF16, torch.float16: FP16}
         codes = (torch.uint8, torch.float8_e4m3fn)
         scales = (torch.uint8, torch.float8_e8m0fnu)
         given = [list(t) if t is not None else [None] * count for t in (params, grads, m, v, m_scale, v_scale, copies)]
         assert all(len(t) == count for t in given), "expected lists of one length"
         params, grads, m, v, m_scale, v_scale, copies = given
         self.state_type = E4M3_BLOCK32 if count and m[0].dtype in codes else FP32
-        self.g_type = real.get(grads[0].dtype if count else torch.float32, -1)
+        self.g_type = _REAL.get(grads[0].dtype if count else torch.float32, -1)
         kinds = {t.dtype for t in copies if t is not None}
         assert len(kinds) <= 1 and kinds <= {torch.bfloat16, torch.float16}, "copies: expected bfloat16 or float16"
-        self.copy_type = real[kinds.pop()] if kinds else BF16
+        self.copy_type = _REAL[kinds.pop()] if kinds else BF16
         self.device = params[0].get_device() if count else None
         assert self.g_type >= 0, "gradients: expected float32, bfloat16 or float16"
         self._table = (_CAdamwTensor * count)()

@@ -21,6 +21,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "fpq_kernels.h"
 
@@ -42,15 +43,6 @@ __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { re
 template <>
 __device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
 
-// 8 (or 4) values side by side, 16-byte (8-byte for 4 16-bit values) aligned
-__device__ __forceinline__ void load_vec(const float* p, float* v, int n)
-{
-#pragma unroll
-    for (int i = 0; i < n; i += 4) {
-        const float4 q = *reinterpret_cast<const float4*>(p + i);
-        v[i] = q.x; v[i + 1] = q.y; v[i + 2] = q.z; v[i + 3] = q.w;
-    }
-}
 __device__ __forceinline__ void unpack(uint32_t w, float* v, __nv_bfloat16)
 {
     v[0] = __uint_as_float(w << 16);
@@ -62,28 +54,66 @@ __device__ __forceinline__ void unpack(uint32_t w, float* v, __half)
     v[0] = f.x;
     v[1] = f.y;
 }
-template <typename T>
-__device__ __forceinline__ void load_vec(const T* p, float* v, int n)
-{
-    if (n == 8) {
-        const uint4 q = *reinterpret_cast<const uint4*>(p);
-        unpack(q.x, v, T()); unpack(q.y, v + 2, T()); unpack(q.z, v + 4, T()); unpack(q.w, v + 6, T());
-    } else {
-        const uint2 q = *reinterpret_cast<const uint2*>(p);
-        unpack(q.x, v, T()); unpack(q.y, v + 2, T());
-    }
-}
 
-// Values [col, col + n) of a row of `width`; those behind its end are zeros.
-template <int n, typename T>
-__device__ __forceinline__ void load_cols(const T* row, int64_t col, int64_t width, bool vec, float* v)
-{
-    if (vec && col + n <= width) {
-        load_vec(row + col, v, n);
-    } else {
+// n values that lie side by side (n = 4 or 8), as they lie: 32-bit words of one FP32 or two 16-bit values.  They are
+// looked into only where they are used: a conversion behind each load would wait for it.
+template <typename T, int n>
+struct Raw {
+    static constexpr int WORDS = n * (int)sizeof(T) / 4;
+    uint32_t w[WORDS];
+
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i)
+            w[i] = 0;
+    }
+    __device__ __forceinline__ void values(float (&v)[n]) const
+    {
 #pragma unroll
         for (int i = 0; i < n; ++i)
-            v[i] = col + i < width ? as_float(row[col + i]) : 0.f;
+            if constexpr (sizeof(T) == 4) {
+                v[i] = __uint_as_float(w[i]);
+            } else if (i % 2 == 0) {
+                unpack(w[i / 2], v + i, T());
+            }
+    }
+};
+
+// Values [col, col + n) of a row of `width`; those behind its end are zeros.  VEC: the row starts at a multiple of 16 bytes
+// (of 8, for four 16-bit values) and its width is a multiple of what a vector holds.
+template <bool VEC, int n, typename T>
+__device__ __forceinline__ void load_cols(const T* row, int64_t col, int64_t width, bool there, Raw<T, n>& r)
+{
+    if constexpr (VEC) {
+        constexpr int PIECE = sizeof(T) == 4 ? 4 : n;
+#pragma unroll
+        for (int i = 0; i < n; i += PIECE) {
+            uint32_t* w = r.w + i * (int)sizeof(T) / 4;
+            if (there && col + i < width) {
+                if constexpr (PIECE * sizeof(T) == 16) {
+                    const uint4 q = *reinterpret_cast<const uint4*>(row + col + i);
+                    w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
+                } else {
+                    const uint2 q = *reinterpret_cast<const uint2*>(row + col + i);
+                    w[0] = q.x; w[1] = q.y;
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < PIECE * (int)sizeof(T) / 4; ++k)
+                    w[k] = 0;
+            }
+        }
+    } else {
+        r.clear();
+#pragma unroll
+        for (int i = 0; i < n; ++i)
+            if (there && col + i < width) {
+                if constexpr (sizeof(T) == 4)
+                    r.w[i] = __float_as_uint(row[col + i]);
+                else
+                    r.w[i / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(row)[col + i] << (16 * (i % 2));
+            }
     }
 }
 
@@ -93,6 +123,18 @@ __device__ __forceinline__ uint32_t low(float x, uint32_t hi) { return __float_a
 __device__ __forceinline__ void mma_tf32(float* c, const uint32_t* a, uint32_t b0, uint32_t b1)
 {
     asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_16(float* c, const uint32_t* a, uint32_t b0, uint32_t b1, __nv_bfloat16)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_16(float* c, const uint32_t* a, uint32_t b0, uint32_t b1, __half)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
@@ -120,6 +162,16 @@ __device__ __forceinline__ void split_four(const float (&v)[4], uint32_t (&h)[4]
     }
 }
 
+// two values as BF16, and what is left of them
+__device__ __forceinline__ void split_bf16(float a, float b, uint32_t& h, uint32_t& l)
+{
+    const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+    const float2 f = __bfloat1622float2(v);
+    const __nv_bfloat162 r = __floats2bfloat162_rn(a - f.x, b - f.y);
+    h = *reinterpret_cast<const uint32_t*>(&v);
+    l = *reinterpret_cast<const uint32_t*>(&r);
+}
+
 template <typename T>
 constexpr bool WIDE = sizeof(T) == 4;
 
@@ -133,8 +185,7 @@ struct TileRows {
     int rows, id;
 };
 
-template <int BM>
-__device__ __forceinline__ TileRows find_tile(int64_t tile, const int32_t* offsets, const int32_t* ids, int S, int G, int64_t M)
+__device__ __forceinline__ TileRows find_tile(int BM, int64_t tile, const int32_t* offsets, const int32_t* ids, int S, int G, int64_t M)
 {
     const int lane = threadIdx.x & 31;
     TileRows r = {0, 0, -1};
@@ -144,7 +195,7 @@ __device__ __forceinline__ TileRows find_tile(int64_t tile, const int32_t* offse
         bool below = false;
         if (s < lo + span) {
             const int64_t o = min(max((int64_t)offsets[s], (int64_t)0), M);
-            below = o / BM + s <= tile;
+            below = (uint32_t)o / (uint32_t)BM + (int64_t)s <= tile;
         }
         const uint32_t votes = __ballot_sync(0xffffffffu, below);
         if (votes == 0)
@@ -156,8 +207,8 @@ __device__ __forceinline__ TileRows find_tile(int64_t tile, const int32_t* offse
             break;
     }
     const int64_t begin = min(max((int64_t)offsets[lo], (int64_t)0), M), end = min(max((int64_t)offsets[lo + 1], (int64_t)0), M);
-    r.row = begin + (tile - (begin / BM + lo)) * BM;
-    r.rows = (int)min((int64_t)BM, end - r.row);
+    r.row = begin + (tile - ((uint32_t)begin / (uint32_t)BM + (int64_t)lo)) * BM;
+    r.rows = (int)max(min((int64_t)BM, end - r.row), (int64_t)0);
     const int id = ids[lo];
     r.id = id >= 0 && id < G ? id : -1;
     return r;
@@ -166,8 +217,8 @@ __device__ __forceinline__ TileRows find_tile(int64_t tile, const int32_t* offse
 // ---- rows to t and back ------------------------------------------------------------------------------------------
 struct RowsArgs {
     const void* in;                // [M][D1], leading dimension ld_in
-    const void* w1;                // reduces:   [G][R][D1], or transposed [G][D1][R]
-    const void* w2;                // expands:   [G][D2][R], or transposed [G][R][D2]
+    const void* w1;                // reduces:   [G][R][D1]
+    const void* w2;                // expands:   [G][D2][R]
     const float* scale;            // [G] or NULL
     const int32_t *offsets, *ids;
     const void* base;              // [M][D2] or NULL
@@ -175,117 +226,119 @@ struct RowsArgs {
     float* kept;                   // [M][R] or NULL: t (forward), s t (backward)
     int64_t M, D1, D2, ld_in, ld_base, ld_out;
     int G, R, S;
-    int vec_in, vec_out, vec_w1, vec_w2;
     int kept_scaled;
+    int wr;                        // row groups of a block: 1, 2, 4 or 8
 };
 
-// The thread's four values per (n-tile, k-pair) of a weight matrix W(n, k): n = row of the MMA's B operand.  Contiguous in k
-// (row pitch ld), or TR: contiguous in n.
-template <bool TR, typename WT>
-__device__ __forceinline__ void load_weights(const WT* w, int64_t n, int64_t N, int64_t k, int64_t K, int64_t ld, bool vec, float (&v)[8])
+// A block has 16 * wr rows; each of its warps takes 16 of them and, with the 8 / wr warps (times the blocks of the cluster) that
+// have the same rows, shares the reduction in groups of 32 columns, then the output in groups of 32 columns.  RP: the rank, padded.
+template <typename XT, typename WT, int RP, bool VEC>
+__global__ void __launch_bounds__(THREADS, RP <= 64 ? 2 : 1) adapter_rows_kernel(const RowsArgs a)
 {
-    if (!TR) {
-        if (n < N)
-            load_cols<8>(w + n * ld, k, K, vec, v);
-        else
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                v[i] = 0.f;
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            v[i] = n < N && k + i < K ? as_float(w[(k + i) * ld + n]) : 0.f;
-    }
-}
-
-// MT: row tiles of 16 in a block; RP: the rank, padded.  The warps (of all blocks of the cluster) share the reduction in
-// groups of 32 columns, then the output in groups of 32 columns.
-template <typename XT, typename WT, int MT, int RP, bool TR>
-__global__ void __launch_bounds__(THREADS) adapter_rows_kernel(const RowsArgs a)
-{
-    constexpr int BM = MT * 16, NT = RP / 8, PITCH = RP == 16 ? 16 : RP + 16;
+    constexpr int NT = RP / 8, PITCH = RP == 16 ? 16 : RP + 16;
+    constexpr bool NATIVE = sizeof(XT) == 2;               // x and weights of one 16-bit type, multiplied as they are
+    constexpr bool AHEAD = RP <= 16;                       // registers for the weights of the next group
     extern __shared__ float4 smem4[];
-    float* parts = reinterpret_cast<float*>(smem4);        // [WARPS][BM][RP], then the block's sum in the first
-    float* t_smem = parts + WARPS * BM * RP;               // [BM][PITCH]
+    float* parts = reinterpret_cast<float*>(smem4);        // [8 / wr][16 wr][RP], then the block's sum in the first
+    float* t_smem = parts + WARPS * 16 * RP;               // [16 wr][PITCH]
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
     uint32_t rank = cluster_rank(), C;
     asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(C));
+    const int WR = a.wr, WK = WARPS / WR, BM = 16 * WR;
     const int64_t tile = blockIdx.x / C;
-    const TileRows tr = find_tile<BM>(tile, a.offsets, a.ids, a.S, a.G, a.M);
+    const TileRows tr = find_tile(BM, tile, a.offsets, a.ids, a.S, a.G, a.M);
     if (tr.rows <= 0)
         return;                                            // (every block of the cluster leaves)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
+    const int r0 = (warp & (WR - 1)) * 16, wk = warp / WR;
     const float s = a.scale && tr.id >= 0 ? a.scale[tr.id] : 1.f;
-    const int64_t D1 = a.D1, D2 = a.D2;
-    const int R = a.R, workers = WARPS * (int)C, worker = (int)rank * WARPS + warp;
-    const XT* in = (const XT*)a.in + tr.row * a.ld_in;
-    const WT* w1 = (const WT*)a.w1 + (int64_t)max(tr.id, 0) * R * D1;
+    const int D1 = (int)a.D1, D2 = (int)a.D2, R = a.R, step = 32 * WK * (int)C, first = 32 * ((int)rank * WK + wk);
     const WT* w2 = (const WT*)a.w2 + (int64_t)max(tr.id, 0) * R * D2;
+    const bool there[2] = {r0 + g < tr.rows, r0 + 8 + g < tr.rows};
 
     if (tr.id >= 0) {
-        float acc[MT][NT][4] = {}, part[MT][NT][4] = {};
+        const XT* in = (const XT*)a.in + tr.row * a.ld_in;
+        const WT* w1 = (const WT*)a.w1 + (int64_t)tr.id * R * D1;
+        const XT* x_row[2] = {in + (r0 + g) * a.ld_in, in + (r0 + 8 + g) * a.ld_in};
+        float acc[NT][4] = {}, part[NT][4] = {};
+        Raw<XT, 8> x[2], x_next[2];
+        Raw<WT, 8> w[NT], w_next[AHEAD ? NT : 1];
         int since = 0;
-        for (int64_t k0 = (int64_t)worker * 32; k0 < D1; k0 += (int64_t)workers * 32) {
-            const int64_t k = k0 + q * 8;
-            float x[MT][2][8];
+        if (r0 < tr.rows && first < D1) {
 #pragma unroll
-            for (int m = 0; m < MT; ++m)
+            for (int h = 0; h < 2; ++h)
+                load_cols<VEC>(x_row[h], first + q * 8, D1, there[h], x_next[h]);
+            if (AHEAD)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int r = m * 16 + h * 8 + g;
-                    if (r < tr.rows)
-                        load_cols<8>(in + r * a.ld_in, k, D1, a.vec_in, x[m][h]);
+                for (int n = 0; n < NT; ++n)
+                    load_cols<VEC>(w1 + (int64_t)(n * 8 + g) * D1, first + q * 8, D1, n * 8 + g < R, w_next[n]);
+            for (int k0 = first; k0 < D1; k0 += step) {
+                x[0] = x_next[0];
+                x[1] = x_next[1];
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+                    if (AHEAD)
+                        w[n] = w_next[n];
                     else
+                        load_cols<VEC>(w1 + (int64_t)(n * 8 + g) * D1, k0 + q * 8, D1, n * 8 + g < R, w[n]);
+                const int k1 = k0 + step + q * 8;          // (behind the end nothing is loaded)
 #pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            x[m][h][i] = 0.f;
-                }
-            float w[NT][8];
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-                load_weights<TR>(w1, n * 8 + g, R, k, D1, TR ? R : D1, a.vec_w1, w[n]);
-#pragma unroll
-            for (int st = 0; st < 4; ++st)
-#pragma unroll
-                for (int m = 0; m < MT; ++m) {
-                    const float v[4] = {x[m][0][2 * st], x[m][1][2 * st], x[m][0][2 * st + 1], x[m][1][2 * st + 1]};
-                    uint32_t vh[4], vl[4];
-                    split_four<WIDE<XT>>(v, vh, vl);
+                for (int h = 0; h < 2; ++h)
+                    load_cols<VEC>(x_row[h], k1, D1, there[h], x_next[h]);
+                if (AHEAD)
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
-                        mma_split<WIDE<XT>, WIDE<WT>>(part[m][n], vh, vl, w[n][2 * st], w[n][2 * st + 1]);
-                }
-            if (++since == 2) {                            // 64 columns
-                since = 0;
+                        load_cols<VEC>(w1 + (int64_t)(n * 8 + g) * D1, k1, D1, n * 8 + g < R, w_next[n]);
+                if constexpr (NATIVE) {
 #pragma unroll
-                for (int m = 0; m < MT; ++m)
+                    for (int st = 0; st < 2; ++st) {
+                        const uint32_t v[4] = {x[0].w[2 * st], x[1].w[2 * st], x[0].w[2 * st + 1], x[1].w[2 * st + 1]};
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+                            mma_16(part[n], v, w[n].w[2 * st], w[n].w[2 * st + 1], XT());
+                    }
+                } else {
+                    float f[2][8], fw[NT][8];
+                    x[0].values(f[0]);
+                    x[1].values(f[1]);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+                        w[n].values(fw[n]);
+#pragma unroll
+                    for (int st = 0; st < 4; ++st) {
+                        const float v[4] = {f[0][2 * st], f[1][2 * st], f[0][2 * st + 1], f[1][2 * st + 1]};
+                        uint32_t vh[4], vl[4];
+                        split_four<true>(v, vh, vl);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+                            mma_split<true, WIDE<WT>>(part[n], vh, vl, fw[n][2 * st], fw[n][2 * st + 1]);
+                    }
+                }
+                if (++since == 2) {                        // 64 columns
+                    since = 0;
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
-                            acc[m][n][i] += part[m][n][i];
-                            part[m][n][i] = 0.f;
+                            acc[n][i] += part[n][i];
+                            part[n][i] = 0.f;
                         }
+                }
             }
         }
-        float* mine = parts + warp * BM * RP;
+        float* mine = parts + (wk * BM + r0) * RP;
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                *reinterpret_cast<float2*>(mine + (m * 16 + g) * RP + n * 8 + 2 * q) =
-                    make_float2(acc[m][n][0] + part[m][n][0], acc[m][n][1] + part[m][n][1]);
-                *reinterpret_cast<float2*>(mine + (m * 16 + 8 + g) * RP + n * 8 + 2 * q) =
-                    make_float2(acc[m][n][2] + part[m][n][2], acc[m][n][3] + part[m][n][3]);
-            }
+        for (int n = 0; n < NT; ++n) {
+            *reinterpret_cast<float2*>(mine + g * RP + n * 8 + 2 * q) = make_float2(acc[n][0] + part[n][0], acc[n][1] + part[n][1]);
+            *reinterpret_cast<float2*>(mine + (8 + g) * RP + n * 8 + 2 * q) = make_float2(acc[n][2] + part[n][2], acc[n][3] + part[n][3]);
+        }
         __syncthreads();
         if (C > 1) {                                       // the block's own sum first: one array per block to fetch
             for (int i = threadIdx.x; i < BM * RP; i += THREADS) {
                 float v = parts[i];
-#pragma unroll
-                for (int k = 1; k < WARPS; ++k)
+                for (int k = 1; k < WK; ++k)
                     v += parts[k * BM * RP + i];
                 parts[i] = v;
             }
@@ -301,14 +354,13 @@ __global__ void __launch_bounds__(THREADS) adapter_rows_kernel(const RowsArgs a)
                     v += p;
                 }
             } else {
-#pragma unroll
-                for (int k = 0; k < WARPS; ++k)
+                for (int k = 0; k < WK; ++k)
                     v += parts[k * BM * RP + i];
             }
             if (!finite(v) && r < tr.rows && j < R) {
                 v = 0.f;
-                for (int64_t k = 0; k < D1; ++k)
-                    v = fmaf(as_float(in[r * a.ld_in + k]), as_float(TR ? w1[k * R + j] : w1[j * D1 + k]), v);
+                for (int k = 0; k < D1; ++k)
+                    v = fmaf(as_float(in[r * a.ld_in + k]), as_float(w1[(int64_t)j * D1 + k]), v);
             }
             if (a.kept && rank == 0 && r < tr.rows && j < R)
                 a.kept[(tr.row + r) * R + j] = a.kept_scaled ? v * s : v;
@@ -322,111 +374,165 @@ __global__ void __launch_bounds__(THREADS) adapter_rows_kernel(const RowsArgs a)
             a.kept[tr.row * R + i] = 0.f;
     }
 
-    if (a.out) {
+    if (a.out && r0 < tr.rows) {
+        // BF16: t in two terms of 8 bits, 2^-17 of it left out against the 2^-9 that y is rounded by; otherwise TF32 terms
+        constexpr bool BF = std::is_same<XT, __nv_bfloat16>::value;
+        constexpr int PER = RP < 32 ? RP / 4 : 8, BLOCKS = RP / (4 * PER);   // ranks of a thread side by side, and how often
+        constexpr bool HOLD = BF || RP <= 32;                                // t's operands stay in registers
         const XT* base = (const XT*)a.base + tr.row * a.ld_base;
         XT* out = (XT*)a.out + tr.row * a.ld_out;
-        for (int64_t c0 = (int64_t)worker * 32; c0 < D2; c0 += (int64_t)workers * 32) {
-            const int64_t col = c0 + q * 8;                // this thread's 8 columns of rows g and g + 8 of every tile
-            float y[MT][2][8];
+        uint32_t th[HOLD ? BLOCKS : 1][PER / 2][4], tl[HOLD ? BLOCKS : 1][PER / 2][4];
+        auto fetch_t = [&](int b, uint32_t (&h)[PER / 2][4], uint32_t (&l)[PER / 2][4]) {
+            float t[2][PER];
 #pragma unroll
-            for (int m = 0; m < MT; ++m)
+            for (int k = 0; k < 2; ++k)
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int r = m * 16 + h * 8 + g;
-                    if (a.base && r < tr.rows)
-                        load_cols<8>(base + r * a.ld_base, col, D2, a.vec_out, y[m][h]);
-                    else
-#pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            y[m][h][i] = 0.f;
+                for (int i = 0; i < PER; i += 4) {
+                    const float4 v = *reinterpret_cast<const float4*>(t_smem + (r0 + k * 8 + g) * PITCH + (b * 4 + q) * PER + i);
+                    t[k][i] = v.x; t[k][i + 1] = v.y; t[k][i + 2] = v.z; t[k][i + 3] = v.w;
                 }
+            if constexpr (BF) {
+#pragma unroll
+                for (int st = 0; st < PER / 4; ++st)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)            // rows g, g + 8, then the second pair of ranks
+                        split_bf16(t[e & 1][4 * st + 2 * (e >> 1)], t[e & 1][4 * st + 2 * (e >> 1) + 1], h[st][e], l[st][e]);
+            } else {
+#pragma unroll
+                for (int st = 0; st < PER / 2; ++st) {
+                    const float v[4] = {t[0][2 * st], t[1][2 * st], t[0][2 * st + 1], t[1][2 * st + 1]};
+                    split_four<true>(v, h[st], l[st]);
+                }
+            }
+        };
+        if constexpr (HOLD)
+            if (tr.id >= 0)
+#pragma unroll
+                for (int b = 0; b < BLOCKS; ++b)
+                    fetch_t(b, th[b], tl[b]);
+        Raw<XT, 8> y0[2];
+        const bool based = a.base != nullptr;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            load_cols<VEC>(base + (r0 + h * 8 + g) * a.ld_base, first + q * 8, D2, based && there[h], y0[h]);
+        for (int c0 = first; c0 < D2; c0 += step) {
+            const int col = c0 + q * 8;                    // this thread's 8 columns of rows g and g + 8
+            float y[2][8], acc[4][4] = {};
             if (tr.id >= 0) {
-                float acc[MT][4][4] = {};
                 // output column of the MMA's column g in tile e: the two columns 2 q and 2 q + 1 that a thread gets of each
                 // of the four tiles are its 8 columns
-                const int64_t n = c0 + 8 * (g >> 1) + (g & 1);
-                constexpr int KG = RP < 32 ? RP : 32;      // ranks at a time
+                const int n = c0 + 8 * (g >> 1) + (g & 1);
 #pragma unroll
-                for (int k0 = 0; k0 < RP; k0 += KG) {
-                    constexpr int PER = KG / 4;            // ranks of a thread: 4 or 8 side by side
-                    float w[4][8];
+                for (int b = 0; b < BLOCKS; ++b) {
+                    Raw<WT, PER> w[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int64_t row = n + 2 * e;
-                        const int k = k0 + q * PER;
+                    for (int e = 0; e < 4; ++e)
+                        load_cols<VEC>(w2 + (int64_t)(n + 2 * e) * R, (b * 4 + q) * PER, R, n + 2 * e < D2, w[e]);
+                    if constexpr (!HOLD)
+                        fetch_t(b, th[0], tl[0]);
+                    const auto& h = th[HOLD ? b : 0];
+                    const auto& l = tl[HOLD ? b : 0];
+                    if constexpr (BF) {
 #pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            w[e][i] = 0.f;
-                        if (row < D2) {
-                            if (!TR)
-                                load_cols<PER>(w2 + row * R, k, R, a.vec_w2, w[e]);
-                            else
+                        for (int st = 0; st < PER / 4; ++st)
 #pragma unroll
-                                for (int i = 0; i < PER; ++i)
-                                    w[e][i] = k + i < R ? as_float(w2[(int64_t)(k + i) * D2 + row]) : 0.f;
-                        }
-                    }
-#pragma unroll
-                    for (int m = 0; m < MT; ++m) {
-                        float t[2][PER];
-#pragma unroll
-                        for (int h = 0; h < 2; ++h)
-                            load_vec(t_smem + (m * 16 + h * 8 + g) * PITCH + k0 + q * PER, t[h], PER);
-#pragma unroll
-                        for (int st = 0; st < PER / 2; ++st) {
-                            const float v[4] = {t[0][2 * st], t[1][2 * st], t[0][2 * st + 1], t[1][2 * st + 1]};
-                            uint32_t vh[4], vl[4];
-                            split_four<true>(v, vh, vl);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                mma_split<true, WIDE<WT>>(acc[m][e], vh, vl, w[e][2 * st], w[e][2 * st + 1]);
-                        }
-                    }
-                }
-#pragma unroll
-                for (int m = 0; m < MT; ++m)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h)
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            float v = acc[m][i >> 1][2 * h + (i & 1)];
-                            const int r = m * 16 + h * 8 + g;
-                            if (!finite(v) && r < tr.rows && col + i < D2) {
-                                v = 0.f;
-                                for (int j = 0; j < R; ++j)
-                                    v = fmaf(t_smem[r * PITCH + j], as_float(TR ? w2[j * D2 + col + i] : w2[(col + i) * R + j]), v);
+                            for (int e = 0; e < 4; ++e) {
+                                mma_16(acc[e], l[st], w[e].w[2 * st], w[e].w[2 * st + 1], __nv_bfloat16());
+                                mma_16(acc[e], h[st], w[e].w[2 * st], w[e].w[2 * st + 1], __nv_bfloat16());
                             }
-                            y[m][h][i] += v;
-                        }
-            }
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int r = m * 16 + h * 8 + g;
-                    if (r >= tr.rows)
-                        continue;
-                    XT* o = out + r * a.ld_out + col;
-                    if (a.vec_out && col + 8 <= D2) {
-                        alignas(16) XT v[8];
-#pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            v[i] = from_float<XT>(y[m][h][i]);
-#pragma unroll
-                        for (int i = 0; i < (int)(8 * sizeof(XT) / 16); ++i)
-                            reinterpret_cast<uint4*>(o)[i] = reinterpret_cast<const uint4*>(v)[i];
                     } else {
 #pragma unroll
-                        for (int i = 0; i < 8; ++i)
-                            if (col + i < D2)
-                                o[i] = from_float<XT>(y[m][h][i]);
+                        for (int e = 0; e < 4; ++e) {
+                            float f[PER];
+                            w[e].values(f);
+#pragma unroll
+                            for (int st = 0; st < PER / 2; ++st)
+                                mma_split<true, WIDE<WT>>(acc[e], h[st], l[st], f[2 * st], f[2 * st + 1]);
+                        }
                     }
                 }
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                y0[h].values(y[h]);
+                load_cols<VEC>(base + (r0 + h * 8 + g) * a.ld_base, col + step, D2, based && there[h], y0[h]);
+            }
+            bool odd = false;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    odd |= !finite(acc[i >> 1][2 * h + (i & 1)]);
+                }
+            if (odd)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        float& v = acc[i >> 1][2 * h + (i & 1)];
+                        const int r = r0 + h * 8 + g;
+                        if (!finite(v) && r < tr.rows && col + i < D2) {
+                            v = 0.f;
+                            for (int j = 0; j < R; ++j)
+                                v = fmaf(t_smem[r * PITCH + j], as_float(w2[(int64_t)(col + i) * R + j]), v);
+                        }
+                    }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    y[h][i] += acc[i >> 1][2 * h + (i & 1)];
+                if (!there[h])
+                    continue;
+                XT* o = out + (r0 + h * 8 + g) * a.ld_out + col;
+                constexpr int PIECE = 16 / (int)sizeof(XT);
+#pragma unroll
+                for (int p = 0; p < 8; p += PIECE) {
+                    if (VEC) {
+                        if (col + p < D2) {
+                            alignas(16) XT v[PIECE];
+#pragma unroll
+                            for (int i = 0; i < PIECE; ++i)
+                                v[i] = from_float<XT>(y[h][p + i]);
+                            *reinterpret_cast<uint4*>(o + p) = *reinterpret_cast<const uint4*>(v);
+                        }
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < PIECE; ++i)
+                            if (col + p + i < D2)
+                                o[p + i] = from_float<XT>(y[h][p + i]);
+                    }
+                }
+            }
         }
     }
     __syncwarp();
     if (C > 1 && tr.id >= 0)
         cluster_wait();                                    // nobody still reads this block's sums
+}
+
+// Adapters transposed for the backward pass: src [G][rows][cols] to dst [G][cols][rows], 32 x 32 at a time.
+template <typename T>
+__global__ void __launch_bounds__(THREADS) transpose_adapters_kernel(const T* a, T* at, const T* b, T* bt, int R, int K, int N, int tiles_a, int tiles)
+{
+    __shared__ T piece[32][33];
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int g = blockIdx.x / tiles, t = blockIdx.x % tiles;
+    const bool is_b = t >= tiles_a;
+    const int rows = is_b ? N : R, cols = is_b ? R : K, across = (cols + 31) / 32, i = is_b ? t - tiles_a : t;
+    const T* src = (is_b ? b : a) + (int64_t)g * rows * cols;
+    T* dst = (is_b ? bt : at) + (int64_t)g * rows * cols;
+    const int x = threadIdx.x & 31, y = threadIdx.x >> 5, r0 = i / across * 32, c0 = i % across * 32;
+#pragma unroll
+    for (int k = y; k < 32; k += 8)
+        if (r0 + k < rows && c0 + x < cols)
+            piece[k][x] = src[(int64_t)(r0 + k) * cols + c0 + x];
+    __syncthreads();
+#pragma unroll
+    for (int k = y; k < 32; k += 8)
+        if (c0 + k < cols && r0 + x < rows)
+            dst[(int64_t)(c0 + k) * rows + r0 + x] = piece[x][k];
 }
 
 // ---- gradients of the adapters -----------------------------------------------------------------------------------
@@ -439,12 +545,12 @@ struct GradArgs {
     const int32_t *offsets, *ids;
     float *da, *db;                // [G][R][K], [G][N][R]
     int64_t M, N, K, ldx, ld_dy;
-    int G, R, S, vec_x, vec_dy;
+    int G, R, S;
     int tiles_k;                   // column tiles of dA; those behind them are dB's
 };
 
 // JT: ranks of a warp; RP / JT warps share a run of rows.
-template <typename XT, int RP, int JT>
+template <typename XT, int RP, int JT, bool VEC>
 __global__ void __launch_bounds__(THREADS) adapter_grad_kernel(const GradArgs a)
 {
     constexpr int NT = JT / 8, WN = RP / JT, WK = WARPS / WN, RUN = 16;
@@ -459,7 +565,6 @@ __global__ void __launch_bounds__(THREADS) adapter_grad_kernel(const GradArgs a)
     const int64_t D = is_b ? a.N : a.K, ld = is_b ? a.ld_dy : a.ldx, c0 = (int64_t)(is_b ? tile - a.tiles_k : tile) * 64;
     const XT* wide = (const XT*)(is_b ? a.dy : a.x);
     const float* thin = is_b ? a.u : a.t;
-    const bool vec = is_b ? a.vec_dy : a.vec_x;
     const int R = a.R, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
     const int wn = warp % WN, wk = warp / WN, workers = WK * (int)C, worker = (int)rank * WK + wk, j0 = wn * JT;
 
@@ -473,40 +578,37 @@ __global__ void __launch_bounds__(THREADS) adapter_grad_kernel(const GradArgs a)
             continue;
         const int64_t n_runs = (end - begin + RUN - 1) / RUN;
         for (int64_t i = (worker - runs + workers) % workers; i < n_runs; i += workers) {
+            // rows of MMA k = q and q + 4; columns 4 g .. of both halves of the tile
+            Raw<XT, 4> v[RUN / 8][2][2];
+            float p[RUN / 8][NT][2];
 #pragma unroll
-            for (int st = 0; st < RUN / 8; ++st) {
-                // rows of MMA k = q and q + 4; columns 4 g .. of both halves of the tile
-                const int64_t r0 = begin + i * RUN + st * 8 + q;
-                float v[2][2][4], p[NT][2];
+            for (int st = 0; st < RUN / 8; ++st)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const int64_t r = r0 + 4 * h;
+                    const int64_t r = begin + i * RUN + st * 8 + q + 4 * h;
 #pragma unroll
                     for (int e = 0; e < 2; ++e)
-#pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            v[h][e][k] = 0.f;
+                        load_cols<VEC>(wide + r * ld, c0 + e * 32 + g * 4, D, r < end, v[st][h][e]);
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
-                        p[n][h] = 0.f;
-                    if (r < end) {
-#pragma unroll
-                        for (int e = 0; e < 2; ++e)
-                            load_cols<4>(wide + r * ld, c0 + e * 32 + g * 4, D, vec, v[h][e]);
-#pragma unroll
-                        for (int n = 0; n < NT; ++n)
-                            if (j0 + n * 8 + g < R)
-                                p[n][h] = thin[r * R + j0 + n * 8 + g];
-                    }
+                        p[st][n][h] = r < end && j0 + n * 8 + g < R ? thin[r * R + j0 + n * 8 + g] : 0.f;
                 }
 #pragma unroll
+            for (int st = 0; st < RUN / 8; ++st) {
+                float f[2][2][4];
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+                        v[st][h][e].values(f[h][e]);
+#pragma unroll
                 for (int m = 0; m < 4; ++m) {              // MMA rows g and g + 8 are columns 4 g + m and 32 + 4 g + m
-                    const float w[4] = {v[0][0][m], v[0][1][m], v[1][0][m], v[1][1][m]};
+                    const float w[4] = {f[0][0][m], f[0][1][m], f[1][0][m], f[1][1][m]};
                     uint32_t wh[4], wl[4];
                     split_four<WIDE<XT>>(w, wh, wl);
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
-                        mma_split<WIDE<XT>, true>(part[m][n], wh, wl, p[n][0], p[n][1]);
+                        mma_split<WIDE<XT>, true>(part[m][n], wh, wl, p[st][n][0], p[st][n][1]);
                 }
             }
             if (++since == 4) {                            // 64 rows
@@ -614,53 +716,58 @@ cudaError_t launch_cluster(void (*kernel)(const Args), std::atomic<uint64_t>& kn
     return cudaLaunchKernelEx(&cfg, kernel, args);
 }
 
-bool vectors(const void* p, int64_t ld, int bytes) { return (uintptr_t)p % 16 == 0 && ld * bytes % 16 == 0; }
+// rows at multiples of 16 bytes, a whole number of vectors long
+bool vectors(const void* p, int64_t ld, int64_t width, int bytes)
+{
+    return (uintptr_t)p % 16 == 0 && ld * bytes % 16 == 0 && width * bytes % 16 == 0;
+}
 
 int type_bytes(int t) { return t == FPQ_FP32 ? 4 : 2; }
 
-template <typename XT, typename WT, int MT, int RP, bool TR>
-cudaError_t launch_rows_as(const RowsArgs& a, cudaStream_t st)
+template <typename XT, typename WT, int RP, bool VEC>
+cudaError_t launch_rows_as(RowsArgs a, cudaStream_t st)
 {
-    constexpr int BM = MT * 16, PITCH = RP == 16 ? 16 : RP + 16;
-    const size_t smem = (size_t)(WARPS * BM * RP + BM * PITCH) * 4;
+    constexpr int PITCH = RP == 16 ? 16 : RP + 16;
+    const int64_t longest = std::max(a.D1, a.out ? a.D2 : 0), groups = (longest + 31) / 32;
+    a.wr = 1;
+    while (a.wr < 8 && a.M / (16 * a.wr) + a.S > 2 * 148 && a.M >= 24 * a.wr * (int64_t)a.S)
+        a.wr *= 2;
+    const int BM = 16 * a.wr;
+    const size_t smem = (size_t)(WARPS * 16 * RP + BM * PITCH) * 4;
     const int64_t tiles = a.M / BM + a.S;
     // clusters until there are two blocks for every SM, while every block has a group of columns for most of its warps
     int c = 1;
-    const int64_t groups = (std::max(a.D1, a.out ? a.D2 : 0) + 31) / 32;
     const int64_t busy = (a.M + BM - 1) / BM + std::min<int64_t>(a.S, a.M) - 1;
-    while (c < 8 && busy * c * 2 <= 2 * 148 && groups > (int64_t)c * WARPS)
+    while (c < 8 && busy * c * 2 <= 2 * 148 && groups > (int64_t)c * (WARPS / a.wr))
         c *= 2;
     static std::atomic<uint64_t> known{0};
-    return launch_cluster<RowsArgs>(adapter_rows_kernel<XT, WT, MT, RP, TR>, known, dim3((unsigned)(tiles * c)), c, smem, st, a);
+    return launch_cluster<RowsArgs>(adapter_rows_kernel<XT, WT, RP, VEC>, known, dim3((unsigned)(tiles * c)), c, smem, st, a);
 }
 
-template <typename XT, typename WT, bool TR>
-cudaError_t launch_rows_rank(const RowsArgs& a, cudaStream_t st)
+template <typename XT, typename WT>
+cudaError_t launch_rows_type(const RowsArgs& a, cudaStream_t st)
 {
-    // row tiles: 32 rows where requests are long enough to fill them
-    const bool tall = a.M >= 24 * (int64_t)a.S;
-    if (a.R <= 16)
-        return tall ? launch_rows_as<XT, WT, 2, 16, TR>(a, st) : launch_rows_as<XT, WT, 1, 16, TR>(a, st);
-    if (a.R <= 32)
-        return tall ? launch_rows_as<XT, WT, 2, 32, TR>(a, st) : launch_rows_as<XT, WT, 1, 32, TR>(a, st);
-    if (a.R <= 64)
-        return launch_rows_as<XT, WT, 1, 64, TR>(a, st);
-    return launch_rows_as<XT, WT, 1, 128, TR>(a, st);
+    const int xb = sizeof(XT), wb = sizeof(WT), ranks = a.R <= 16 ? 4 : 8;
+    const bool vec = vectors(a.in, a.ld_in, a.D1, xb) && vectors(a.w1, a.D1, a.D1, wb) &&
+                     (!a.out || (vectors(a.out, a.ld_out, a.D2, xb) && (!a.base || vectors(a.base, a.ld_base, a.D2, xb)) &&
+                                 a.R % ranks == 0 && (uintptr_t)a.w2 % 16 == 0));
+#define FPQ_ROWS(RP) (vec ? launch_rows_as<XT, WT, RP, true>(a, st) : launch_rows_as<XT, WT, RP, false>(a, st))
+    return a.R <= 16 ? FPQ_ROWS(16) : a.R <= 32 ? FPQ_ROWS(32) : a.R <= 64 ? FPQ_ROWS(64) : FPQ_ROWS(128);
+#undef FPQ_ROWS
 }
 
-template <bool TR>
 cudaError_t launch_rows(const RowsArgs& a, int x_type, int w_type, cudaStream_t st)
 {
     if (x_type == FPQ_BF16)
-        return launch_rows_rank<__nv_bfloat16, __nv_bfloat16, TR>(a, st);
+        return launch_rows_type<__nv_bfloat16, __nv_bfloat16>(a, st);
     if (x_type == FPQ_FP16)
-        return launch_rows_rank<__half, __half, TR>(a, st);
-    return w_type == FPQ_FP32   ? launch_rows_rank<float, float, TR>(a, st)
-           : w_type == FPQ_BF16 ? launch_rows_rank<float, __nv_bfloat16, TR>(a, st)
-                                : launch_rows_rank<float, __half, TR>(a, st);
+        return launch_rows_type<__half, __half>(a, st);
+    return w_type == FPQ_FP32   ? launch_rows_type<float, float>(a, st)
+           : w_type == FPQ_BF16 ? launch_rows_type<float, __nv_bfloat16>(a, st)
+                                : launch_rows_type<float, __half>(a, st);
 }
 
-template <typename XT, int RP, int JT>
+template <typename XT, int RP, int JT, bool VEC>
 cudaError_t launch_grad_as(const GradArgs& a, int tiles, cudaStream_t st)
 {
     const size_t smem = (size_t)(WARPS / (RP / JT)) * 64 * RP * 4;
@@ -668,58 +775,72 @@ cudaError_t launch_grad_as(const GradArgs& a, int tiles, cudaStream_t st)
     while (c < 8 && (int64_t)tiles * a.G * c * 2 <= 3 * 148 && a.M > (int64_t)c * 128)
         c *= 2;
     static std::atomic<uint64_t> known{0};
-    return launch_cluster<GradArgs>(adapter_grad_kernel<XT, RP, JT>, known, dim3((unsigned)(tiles * c), (unsigned)a.G), c, smem, st, a);
+    return launch_cluster<GradArgs>(adapter_grad_kernel<XT, RP, JT, VEC>, known, dim3((unsigned)(tiles * c), (unsigned)a.G), c, smem, st, a);
 }
 
 template <typename XT>
 cudaError_t launch_grad(const GradArgs& a, int tiles, cudaStream_t st)
 {
-    return a.R <= 16   ? launch_grad_as<XT, 16, 16>(a, tiles, st)
-           : a.R <= 32 ? launch_grad_as<XT, 32, 32>(a, tiles, st)
-           : a.R <= 64 ? launch_grad_as<XT, 64, 32>(a, tiles, st)
-                       : launch_grad_as<XT, 128, 32>(a, tiles, st);
+    const bool vec = vectors(a.x, a.ldx, a.K, sizeof(XT)) && vectors(a.dy, a.ld_dy, a.N, sizeof(XT));
+#define FPQ_GRAD(RP, JT) (vec ? launch_grad_as<XT, RP, JT, true>(a, tiles, st) : launch_grad_as<XT, RP, JT, false>(a, tiles, st))
+    return a.R <= 16 ? FPQ_GRAD(16, 16) : a.R <= 32 ? FPQ_GRAD(32, 32) : a.R <= 64 ? FPQ_GRAD(64, 32) : FPQ_GRAD(128, 32);
+#undef FPQ_GRAD
 }
+
+template <typename T>
+cudaError_t launch_transpose_as(const AdapterProblem& p, T* at, T* bt, cudaStream_t st)
+{
+    const int64_t r = (p.R + 31) / 32, tiles_a = r * ((p.K + 31) / 32), tiles = tiles_a + r * ((p.N + 31) / 32);
+    return launch_overlapped(transpose_adapters_kernel<T>, dim3((unsigned)(tiles * p.G)), THREADS, 0, st, (const T*)p.a, at, (const T*)p.b, bt,
+                             p.R, (int)p.K, (int)p.N, (int)tiles_a, (int)tiles);
+}
+
+size_t pad16(size_t n) { return (n + 15) / 16 * 16; }
 
 }  // namespace
 
 cudaError_t launch_adapter_forward(const AdapterProblem& p, const void* x, int64_t ldx, const void* base, int64_t ld_base, void* y,
                                    int64_t ldy, float* u, cudaStream_t st)
 {
-    const int xb = type_bytes(p.x_type), wb = type_bytes(p.w_type);
     RowsArgs a = {};
     a.in = x; a.w1 = p.a; a.w2 = p.b; a.scale = p.scale; a.offsets = p.offsets; a.ids = p.ids;
     a.base = base; a.out = y; a.kept = u;
     a.M = p.M; a.D1 = p.K; a.D2 = p.N; a.ld_in = ldx; a.ld_base = ld_base; a.ld_out = ldy;
     a.G = p.G; a.R = p.R; a.S = p.S;
-    a.vec_in = vectors(x, ldx, xb);
-    a.vec_out = vectors(y, ldy, xb) && (!base || vectors(base, ld_base, xb));
-    a.vec_w1 = vectors(p.a, p.K, wb);
-    a.vec_w2 = vectors(p.b, p.R, wb);
-    return launch_rows<false>(a, p.x_type, p.w_type, st);
+    return launch_rows(a, p.x_type, p.w_type, st);
+}
+
+// workspace: t [M][R] FP32, then A and B transposed
+size_t adapter_backward_bytes(int64_t M, int64_t N, int64_t K, int G, int R, int w_type)
+{
+    const size_t wb = type_bytes(w_type), g = (size_t)G * R * wb;
+    return pad16((size_t)M * R * 4) + pad16(g * K) + pad16(g * N);
 }
 
 cudaError_t launch_adapter_backward(const AdapterProblem& p, const void* dy, int64_t ld_dy, const void* x, int64_t ldx, const float* u,
-                                    const void* base, int64_t ld_base, void* dx, int64_t ld_dx, float* da, float* db, float* t,
+                                    const void* base, int64_t ld_base, void* dx, int64_t ld_dx, float* da, float* db, void* workspace,
                                     cudaStream_t st)
 {
-    const int xb = type_bytes(p.x_type);
+    float* t = (float*)workspace;
     if (p.M > 0 && p.S > 0) {
+        uint8_t* at = (uint8_t*)workspace + pad16((size_t)p.M * p.R * 4);
+        uint8_t* bt = at + pad16((size_t)p.G * p.R * p.K * type_bytes(p.w_type));
+        cudaError_t e = type_bytes(p.w_type) == 4 ? launch_transpose_as(p, (uint32_t*)at, (uint32_t*)bt, st)
+                                                  : launch_transpose_as(p, (uint16_t*)at, (uint16_t*)bt, st);
+        if (e != cudaSuccess)
+            return e;
         RowsArgs a = {};
-        a.in = dy; a.w1 = p.b; a.w2 = p.a; a.scale = p.scale; a.offsets = p.offsets; a.ids = p.ids;
+        a.in = dy; a.w1 = bt; a.w2 = at; a.scale = p.scale; a.offsets = p.offsets; a.ids = p.ids;
         a.base = base; a.out = dx; a.kept = t; a.kept_scaled = 1;
         a.M = p.M; a.D1 = p.N; a.D2 = p.K; a.ld_in = ld_dy; a.ld_base = ld_base; a.ld_out = ld_dx;
         a.G = p.G; a.R = p.R; a.S = p.S;
-        a.vec_in = vectors(dy, ld_dy, xb);
-        a.vec_out = dx && vectors(dx, ld_dx, xb) && (!base || vectors(base, ld_base, xb));
-        const cudaError_t e = launch_rows<true>(a, p.x_type, p.w_type, st);
+        e = launch_rows(a, p.x_type, p.w_type, st);
         if (e != cudaSuccess)
             return e;
     }
     GradArgs b = {};
     b.x = x; b.dy = dy; b.t = t; b.u = u; b.scale = p.scale; b.offsets = p.offsets; b.ids = p.ids; b.da = da; b.db = db;
     b.M = p.M; b.N = p.N; b.K = p.K; b.ldx = ldx; b.ld_dy = ld_dy; b.G = p.G; b.R = p.R; b.S = p.M > 0 ? p.S : 0;
-    b.vec_x = vectors(x, ldx, xb);
-    b.vec_dy = vectors(dy, ld_dy, xb);
     b.tiles_k = (int)((p.K + 63) / 64);
     const int tiles = b.tiles_k + (int)((p.N + 63) / 64);
     return p.x_type == FPQ_FP32   ? launch_grad<float>(b, tiles, st)

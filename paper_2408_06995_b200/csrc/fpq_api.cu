@@ -1474,11 +1474,10 @@ fpq_status fpq_adapter_forward(const void* x, int64_t ldx, int32_t x_type, const
     return launch_adapter_forward(p, x, ldx, base, ld_base, y, ldy, u, (cudaStream_t)stream) == cudaSuccess ? FPQ_OK : FPQ_ERR_CUDA;
 }
 
-size_t fpq_adapter_backward_workspace_size(int64_t M, int32_t R)
+size_t fpq_adapter_backward_workspace_size(int64_t M, int64_t N, int64_t K, int32_t G, int32_t R, int32_t w_type)
 {
-    if (M < 0 || M > 0x7fffffff || R < 1 || R > 128)
-        return 0;
-    return (size_t)M * (size_t)R * 4 + 16;
+    const AdapterProblem p = {nullptr, nullptr, nullptr, nullptr, nullptr, FPQ_FP32, w_type, G, R, 0, M, N, K};
+    return check_adapters(p) == FPQ_OK ? adapter_backward_bytes(M, N, K, G, R, w_type) : 0;
 }
 
 fpq_status fpq_adapter_backward(const void* dy, int64_t ld_dy, const void* x, int64_t ldx, int32_t x_type, const float* u,
@@ -1506,10 +1505,10 @@ fpq_status fpq_adapter_backward(const void* dy, int64_t ld_dy, const void* x, in
         const size_t xb = real_bytes(x_type);
         if (!aligned(dy, xb) || !aligned(x, xb) || !aligned(dx, xb) || !aligned(base, xb) || !aligned(u, 4) || !aligned(workspace, 16))
             return FPQ_ERR_ALIGN;
-        if (!workspace || ws_bytes < fpq_adapter_backward_workspace_size(M, R))
+        if (!workspace || ws_bytes < adapter_backward_bytes(M, N, K, G, R, w_type))
             return FPQ_ERR_WORKSPACE;
     }
-    return launch_adapter_backward(p, dy, ld_dy, x, ldx, u, dx ? base : nullptr, ld_base, dx, ld_dx, da, db, (float*)workspace,
+    return launch_adapter_backward(p, dy, ld_dy, x, ldx, u, dx ? base : nullptr, ld_base, dx, ld_dx, da, db, workspace,
                                    (cudaStream_t)stream) == cudaSuccess ? FPQ_OK : FPQ_ERR_CUDA;
 }
 

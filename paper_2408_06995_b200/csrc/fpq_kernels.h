@@ -167,7 +167,7 @@ struct GeneralLayer {
 size_t general_layer_workspace_bytes(const GeneralLayer& g);
 fpq_status launch_general_layer(const GeneralLayer& g, void* workspace, cudaStream_t st);
 
-// Low-rank adapters (t: [M][R] scratch that receives s B^T dy), and the AdamW step; arguments checked by the callers.
+// Low-rank adapters and the AdamW step; arguments checked by the callers.
 struct AdapterProblem {
     const void *a, *b;        // [G][R][K], [G][N][R]
     const float* scale;       // [G] or NULL
@@ -178,8 +178,9 @@ struct AdapterProblem {
 cudaError_t launch_adapter_forward(const AdapterProblem& p, const void* x, int64_t ldx, const void* base, int64_t ld_base, void* y,
                                    int64_t ldy, float* u, cudaStream_t st);
 cudaError_t launch_adapter_backward(const AdapterProblem& p, const void* dy, int64_t ld_dy, const void* x, int64_t ldx, const float* u,
-                                    const void* base, int64_t ld_base, void* dx, int64_t ld_dx, float* da, float* db, float* t,
+                                    const void* base, int64_t ld_base, void* dx, int64_t ld_dx, float* da, float* db, void* workspace,
                                     cudaStream_t st);
+size_t adapter_backward_bytes(int64_t M, int64_t N, int64_t K, int G, int R, int w_type);
 fpq_status launch_adamw(const fpq_adamw_tensor* t, int count, int g_type, int copy_type, int state_type, const fpq_adamw_options& o,
                         const float* factors, int64_t* step, cudaStream_t st);
 

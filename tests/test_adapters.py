@@ -11,6 +11,9 @@ fpq_build.build()
 F32, BF, HF = torch.float32, torch.bfloat16, torch.float16
 
 
+WS = 10 * 4 * 4 + 2 * 4 * (16 + 8) * 4          # t [M][R], A and B transposed
+
+
 # ---- refusals, without a GPU ------------------------------------------------------------------------------------------
 
 class Call:
@@ -23,7 +26,7 @@ class Call:
     def __init__(self, **given):
         pointers = {k: 4096 for k in ("x", "a", "b", "scale", "offsets", "ids", "base", "y", "u", "dy", "dx", "da", "db", "workspace")}
         self.v = {**pointers, "x_type": fpq.FP32, "w_type": fpq.FP32, "G": 2, "R": 4, "S": 3, "M": 10, "N": 8, "K": 16, "ldx": 16, "ldy": 8,
-                  "ld_base": 8, "ld_dy": 8, "ld_dx": 16, "ws_bytes": 10 * 4 * 4 + 16, "stream": None, **given}
+                  "ld_base": 8, "ld_dy": 8, "ld_dx": 16, "ws_bytes": WS, "stream": None, **given}
 
     def run(self, name):
         return getattr(fpq.lib(), "fpq_adapter_" + name)(*[self.v[k] for k in getattr(self, name)])
@@ -49,7 +52,7 @@ def test_forward_refuses(given, error):
                                                ({"db": None}, "ERR_NULL"), ({"dy": 4098}, "ERR_ALIGN"), ({"da": 4098}, "ERR_ALIGN"),
                                                ({"dx": 4098}, "ERR_ALIGN"), ({"workspace": 4100}, "ERR_ALIGN"), ({"ld_dy": 7}, "ERR_SHAPE"),
                                                ({"ld_dx": 15}, "ERR_SHAPE"), ({"ld_base": 15}, "ERR_SHAPE"), ({"workspace": None}, "ERR_WORKSPACE"),
-                                               ({"ws_bytes": 10 * 4 * 4 + 15}, "ERR_WORKSPACE")])
+                                               ({"ws_bytes": WS - 1}, "ERR_WORKSPACE")])
 def test_backward_refuses(given, error):
     assert Call(**{"ld_base": 16, "N": 8, **({"ld_dy": given["N"]} if "N" in given and given["N"] > 8 else {}), **given}).run("backward") == getattr(fpq, error)
 
@@ -60,8 +63,10 @@ def test_nothing_to_do_is_no_error():
 
 
 def test_workspace_size():
-    assert fpq.fpq_adapter_backward_workspace_size(1000, 16) >= 1000 * 16 * 4
-    assert fpq.fpq_adapter_backward_workspace_size(-1, 16) == 0 and fpq.fpq_adapter_backward_workspace_size(10, 129) == 0
+    assert fpq.fpq_adapter_backward_workspace_size(10, 8, 16, 2, 4, fpq.FP32) == WS
+    assert fpq.fpq_adapter_backward_workspace_size(-1, 8, 16, 2, 4, fpq.FP32) == 0
+    assert fpq.fpq_adapter_backward_workspace_size(10, 8, 16, 2, 129, fpq.FP32) == 0
+    assert fpq.fpq_adapter_backward_workspace_size(10, 8, 16, 2, 4, 3) == 0
 
 
 def test_binding_takes_no_cpu_tensors():
@@ -104,13 +109,15 @@ def half_step(t, v):
     return torch.finfo(t).eps / 2 * v.abs() + tiny / 2
 
 
-def rows_exact(x, w1, w2, base, s, R):
-    """t, y and their error bounds for the rows of one adapter: t = x w1^T, y = base + s t w2^T."""
+def rows_exact(x, w1, w2, base, s, R, xt=F32):
+    """t, y and their error bounds for the rows of one adapter: t = x w1^T, y = base + s t w2^T.  With BF16 operands t is multiplied as two
+    BF16 terms: the first is off by 2^-9 of t at most, the second by 2^-9 of that."""
     D1 = x.shape[1]
     t = x @ w1.T
     dt = product_error(D1, 24) * (x.abs() @ w1.abs().T)
     y = s * (t @ w2.T)
-    dy = s * (dt @ w2.abs().T + (product_error(R, 3 * R / 8) + 2.0 ** -23) * (t.abs() @ w2.abs().T))
+    split = 2.0 ** -18 if xt == BF else 0.0
+    dy = s * (dt @ w2.abs().T + (product_error(R, 3 * R / 8) + 2.0 ** -23 + split) * (t.abs() @ w2.abs().T))
     if base is not None:
         y = y + base
     return t, dt, y, dy + 2.0 ** -23 * y.abs()
@@ -143,7 +150,7 @@ def check_forward(t, before, y, u, base=True):
             assert torch.equal(y[lo:hi], t["base"][lo:hi] if base else torch.zeros_like(y[lo:hi])) and not bool(u[lo:hi].any())
             continue
         s = float(t["scale"][i]) if t["scale"] is not None else 1.0
-        te, dt, ye, dy = rows_exact(t["x"][lo:hi].double(), t["a"][i].double(), t["b"][i].double(), b0, s, u.shape[1])
+        te, dt, ye, dy = rows_exact(t["x"][lo:hi].double(), t["a"][i].double(), t["b"][i].double(), b0, s, u.shape[1], y.dtype)
         check_rows(u[lo:hi], te, dt, "u")
         check_rows(y[lo:hi], ye, dy, "y")
     assert torch.equal(y[~inside], before[~inside]) and bool((u[~inside] == -7).all())
@@ -245,7 +252,7 @@ def test_replayed_with_other_segments():
     t = make(120, 320, 64, 16, [0, 50, 120], [0, 1], 3)
     y, u = torch.zeros(120, 64, device="cuda"), torch.zeros(120, 16, device="cuda")
     da, db, dx = torch.zeros_like(t["a"]), torch.zeros_like(t["b"]), torch.zeros(120, 320, device="cuda")
-    ws = torch.empty(fpq.fpq_adapter_backward_workspace_size(120, 16), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(fpq.fpq_adapter_backward_workspace_size(120, 64, 320, 3, 16, fpq.FP32), dtype=torch.uint8, device="cuda")
 
     def both():
         fpq.fpq_adapter_forward(t["x"], t["a"], t["b"], t["offsets"], t["ids"], t["scale"], t["base"], y, u)
@@ -284,7 +291,7 @@ def check_backward(t, u, dx, da, db, before, base=True, have_dx=True):
             continue
         s = float(t["scale"][i]) if t["scale"] is not None else 1.0
         dy, x, uu = t["dy"][lo:hi].double(), t["x"][lo:hi].double(), u[lo:hi].double()
-        te, dt, xe, dxe = rows_exact(dy, t["b"][i].double().T, t["a"][i].double().T, b0, s, R)
+        te, dt, xe, dxe = rows_exact(dy, t["b"][i].double().T, t["a"][i].double().T, b0, s, R, t["x"].dtype)
         if have_dx:
             check_rows(dx[lo:hi], xe, dxe, "dx")
         te, dt = s * te, s * dt + 2.0 ** -23 * s * te.abs()
