@@ -139,16 +139,42 @@ __device__ __forceinline__ void mma_16(float* c, const uint32_t* a, uint32_t b0,
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// c += a b with FP32 operands in two terms each (SPLIT_A / SPLIT_B: the operand has more bits than TF32)
-template <bool SPLIT_A, bool SPLIT_B>
-__device__ __forceinline__ void mma_split(float* c, const uint32_t* ah, const uint32_t* al, float b0, float b1)
+// c = a b
+__device__ __forceinline__ void mma_tf32_from_zero(float* c, const uint32_t* a, uint32_t b0, uint32_t b1)
 {
-    const uint32_t h0 = SPLIT_B ? high(b0) : __float_as_uint(b0), h1 = SPLIT_B ? high(b1) : __float_as_uint(b1);
+    asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+                 : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
+__device__ __forceinline__ void mma_16_from_zero(float* c, const uint32_t* a, uint32_t b0, uint32_t b1)
+{
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+                 : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
+
+// c[n] += a b[n] for N tiles, FP32 operands in two terms each (SPLIT_A / SPLIT_B: the operand has more bits than TF32).  One
+// term after the other over all tiles: an MMA that waits for the one in front takes four times as long.
+template <bool SPLIT_A, bool SPLIT_B, int N>
+__device__ __forceinline__ void mma_split(float (*c)[4], const uint32_t* ah, const uint32_t* al, const float (&b)[N][2])
+{
+    uint32_t h[N][2];
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            h[n][k] = SPLIT_B ? high(b[n][k]) : __float_as_uint(b[n][k]);
     if (SPLIT_B)
-        mma_tf32(c, ah, low(b0, h0), low(b1, h1));
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+            mma_tf32(c[n], ah, low(b[n][0], h[n][0]), low(b[n][1], h[n][1]));
     if (SPLIT_A)
-        mma_tf32(c, al, h0, h1);
-    mma_tf32(c, ah, h0, h1);
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+            mma_tf32(c[n], al, h[n][0], h[n][1]);
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+        mma_tf32(c[n], ah, h[n][0], h[n][1]);
 }
 
 template <bool SPLIT>
@@ -311,9 +337,13 @@ __global__ void __launch_bounds__(THREADS, RP <= 64 ? 2 : 1) adapter_rows_kernel
                         const float v[4] = {f[0][2 * st], f[1][2 * st], f[0][2 * st + 1], f[1][2 * st + 1]};
                         uint32_t vh[4], vl[4];
                         split_four<true>(v, vh, vl);
+                        float b[NT][2];
 #pragma unroll
-                        for (int n = 0; n < NT; ++n)
-                            mma_split<true, WIDE<WT>>(part[n], vh, vl, fw[n][2 * st], fw[n][2 * st + 1]);
+                        for (int n = 0; n < NT; ++n) {
+                            b[n][0] = fw[n][2 * st];
+                            b[n][1] = fw[n][2 * st + 1];
+                        }
+                        mma_split<true, WIDE<WT>, NT>(part, vh, vl, b);
                     }
                 }
                 if (++since == 2) {                        // 64 columns
@@ -435,19 +465,20 @@ __global__ void __launch_bounds__(THREADS, RP <= 64 ? 2 : 1) adapter_rows_kernel
                     if constexpr (BF) {
 #pragma unroll
                         for (int st = 0; st < PER / 4; ++st)
+                            for (int k = 0; k < 2; ++k)
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                mma_16(acc[e], l[st], w[e].w[2 * st], w[e].w[2 * st + 1], __nv_bfloat16());
-                                mma_16(acc[e], h[st], w[e].w[2 * st], w[e].w[2 * st + 1], __nv_bfloat16());
-                            }
+                                for (int e = 0; e < 4; ++e)
+                                    mma_16(acc[e], k ? h[st] : l[st], w[e].w[2 * st], w[e].w[2 * st + 1], __nv_bfloat16());
                     } else {
+                        float f[4][PER];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            float f[PER];
-                            w[e].values(f);
+                        for (int e = 0; e < 4; ++e)
+                            w[e].values(f[e]);
 #pragma unroll
-                            for (int st = 0; st < PER / 2; ++st)
-                                mma_split<true, WIDE<WT>>(acc[e], h[st], l[st], f[2 * st], f[2 * st + 1]);
+                        for (int st = 0; st < PER / 2; ++st) {
+                            const float v[4][2] = {{f[0][2 * st], f[0][2 * st + 1]}, {f[1][2 * st], f[1][2 * st + 1]},
+                                                   {f[2][2 * st], f[2][2 * st + 1]}, {f[3][2 * st], f[3][2 * st + 1]}};
+                            mma_split<true, WIDE<WT>, 4>(acc, h[st], l[st], v);
                         }
                     }
                 }
@@ -537,7 +568,8 @@ __global__ void __launch_bounds__(THREADS) transpose_adapters_kernel(const T* a,
 
 // ---- gradients of the adapters -----------------------------------------------------------------------------------
 // out(col, j) = sum over an adapter's rows of wide[i][col] * thin[i][j]: columns of x with t (dA) and of dy with u (dB).  A
-// block takes 64 columns; its warps, and the blocks of its cluster, share the rows in runs of 16 and add up in a fixed order.
+// block takes 64 columns; its warps, and the blocks with the same columns, share the rows in runs.  Sums are added up in a fixed
+// order: those of the warps in shared memory, those of the blocks by a kernel behind this one.
 struct GradArgs {
     const void *x, *dy;
     const float *t, *u;            // [M][R]
@@ -546,140 +578,329 @@ struct GradArgs {
     float *da, *db;                // [G][R][K], [G][N][R]
     int64_t M, N, K, ldx, ld_dy;
     int G, R, S;
-    int tiles_k;                   // column tiles of dA; those behind them are dB's
+    int tiles_k, tiles;            // column tiles of dA; those behind them are dB's
+    float* sums;                   // [split][G][tiles][64 RP] where the rows are split
+    int splits;
 };
 
-// JT: ranks of a warp; RP / JT warps share a run of rows.
-template <typename XT, int RP, int JT, bool VEC>
-__global__ void __launch_bounds__(THREADS) adapter_grad_kernel(const GradArgs a)
+// Element i of a tile's 64 RP, in the order of the output's contiguous side.
+__device__ __forceinline__ void tile_element(int i, int RP, bool is_b, int& col, int& j)
 {
-    constexpr int NT = JT / 8, WN = RP / JT, WK = WARPS / WN, RUN = 16;
-    extern __shared__ float4 smem4[];
-    float* parts = reinterpret_cast<float*>(smem4);        // [WK][64][RP]
+    col = is_b ? i / RP : i % 64;
+    j = is_b ? i % RP : i / 64;
+}
+
+template <typename XT>
+__device__ __forceinline__ void store_gradient(const GradArgs& a, int id, bool is_b, int64_t col, int j, float v)
+{
+    if (!finite(v)) {
+        const XT* wide = (const XT*)(is_b ? a.dy : a.x) + col;
+        const float* thin = (is_b ? a.u : a.t) + j;
+        const int64_t ld = is_b ? a.ld_dy : a.ldx;
+        v = 0.f;
+        for (int sg = 0; sg < a.S; ++sg) {
+            if (a.ids[sg] != id)
+                continue;
+            const int64_t begin = min(max((int64_t)a.offsets[sg], (int64_t)0), a.M), end = min(max((int64_t)a.offsets[sg + 1], (int64_t)0), a.M);
+            for (int64_t r = begin; r < end; ++r)
+                v = fmaf(as_float(wide[r * ld]), thin[r * a.R], v);
+        }
+    }
+    if (is_b)
+        a.db[((int64_t)id * a.N + col) * a.R + j] = a.scale ? v * a.scale[id] : v;
+    else
+        a.da[((int64_t)id * a.R + j) * a.K + col] = v;
+}
+
+template <typename XT>
+__global__ void __launch_bounds__(THREADS) adapter_grad_sum_kernel(const GradArgs a, int RP)
+{
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    uint32_t rank = cluster_rank(), C;
-    asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(C));
-    const int tile = blockIdx.x / C, id = blockIdx.y;
+    const int per = 64 * RP / THREADS, tile = blockIdx.x / per, id = blockIdx.y, i = blockIdx.x % per * THREADS + threadIdx.x;
+    const bool is_b = tile >= a.tiles_k;
+    int col, j;
+    tile_element(i, RP, is_b, col, j);
+    col += (is_b ? tile - a.tiles_k : tile) * 64;
+    if (col >= (is_b ? a.N : a.K) || j >= a.R)
+        return;
+    const int64_t step = (int64_t)a.G * a.tiles * 64 * RP;
+    const float* s = a.sums + ((int64_t)id * a.tiles + tile) * 64 * RP + i;
+    float v = 0.f;
+#pragma unroll 8
+    for (int z = 0; z < a.splits; ++z)
+        v += s[z * step];
+    store_gradient<XT>(a, id, is_b, col, j, v);
+}
+
+__device__ __forceinline__ void copy_async16(uint32_t dst, const void* src, bool there)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copy_async4(uint32_t dst, const void* src, bool there)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(there ? 4 : 0) : "memory");
+}
+
+// Every warp has a ring of its own in shared memory: runs of 16 (32) rows of 64 columns and of its JT ranks, fetched
+// asynchronously STAGES - 1 runs ahead; no warp waits for another before the end.  The pitches keep a quarter warp's
+// vectors, and a warp's single words, in different banks.
+template <typename XT, int JT>
+struct GradRing {
+    static constexpr int RUN = sizeof(XT) == 2 && JT == 16 ? 32 : 16;
+    static constexpr int WIDE_PITCH = 64 * (int)sizeof(XT) + 16, THIN_PITCH = (JT + 4) * 4;      // bytes
+    static constexpr int STAGE = RUN * (WIDE_PITCH + THIN_PITCH);
+    static constexpr int STAGES = sizeof(XT) == 2 && JT == 32 ? 3 : 2;                            // two blocks on an SM
+};
+
+// JT: ranks of a warp; RP / JT warps share a run of rows.  VEC: rows of x and dy by 16 bytes; the thin rows by 16 bytes if R % 4 == 0.
+template <typename XT, int RP, int JT, bool VEC>
+__global__ void __launch_bounds__(THREADS, 2) adapter_grad_kernel(const GradArgs a)
+{
+    using Ring = GradRing<XT, JT>;
+    constexpr int NT = JT / 8, WN = RP / JT, WK = WARPS / WN, RUN = Ring::RUN, STAGES = Ring::STAGES;
+    constexpr int MB = 4 / NT < 1 ? 1 : 4 / NT;            // four independent MMAs one after the other
+    extern __shared__ float4 smem4[];
+    float* parts = reinterpret_cast<float*>(smem4);        // at the end: [WK][64][RP]
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int tile = blockIdx.x, id = blockIdx.y;
     const bool is_b = tile >= a.tiles_k;
     const int64_t D = is_b ? a.N : a.K, ld = is_b ? a.ld_dy : a.ldx, c0 = (int64_t)(is_b ? tile - a.tiles_k : tile) * 64;
     const XT* wide = (const XT*)(is_b ? a.dy : a.x);
     const float* thin = is_b ? a.u : a.t;
     const int R = a.R, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
-    const int wn = warp % WN, wk = warp / WN, workers = WK * (int)C, worker = (int)rank * WK + wk, j0 = wn * JT;
+    const int wn = warp % WN, wk = warp / WN, workers = WK * (int)gridDim.z, worker = (int)blockIdx.z * WK + wk, j0 = wn * JT;
+    uint8_t* ring = reinterpret_cast<uint8_t*>(smem4) + warp * (STAGES * Ring::STAGE);
 
-    float acc[4][NT][4] = {}, part[4][NT][4] = {};
-    int since = 0, runs = 0;                               // runs of the segments in front, modulo the workers
-    for (int sg = 0; sg < a.S; ++sg) {
-        if (a.ids[sg] != id)
-            continue;
-        const int64_t begin = min(max((int64_t)a.offsets[sg], (int64_t)0), a.M), end = min(max((int64_t)a.offsets[sg + 1], (int64_t)0), a.M);
-        if (end <= begin)
-            continue;
-        const int64_t n_runs = (end - begin + RUN - 1) / RUN;
-        for (int64_t i = (worker - runs + workers) % workers; i < n_runs; i += workers) {
-            // rows of MMA k = q and q + 4; columns 4 g .. of both halves of the tile
-            Raw<XT, 4> v[RUN / 8][2][2];
-            float p[RUN / 8][NT][2];
+    // the runs of this warp, in order: every workers-th of all runs of the adapter's segments
+    int sg = -1, runs = 0;                                 // runs of the segments in front, modulo the workers
+    int at = 0, n_runs = 0, begin = 0, end = 0;
+    auto next_run = [&](int& row, int& rows) {
+        while (at >= n_runs) {
+            runs = (runs + n_runs) % workers;
+            n_runs = 0;
+            do
+                if (++sg >= a.S)
+                    return false;
+            while (a.ids[sg] != id);
+            begin = min(max(a.offsets[sg], 0), (int)a.M);
+            end = min(max(a.offsets[sg + 1], 0), (int)a.M);
+            n_runs = end > begin ? (end - begin - 1) / RUN + 1 : 0;
+            at = worker - runs + (worker < runs ? workers : 0);
+        }
+        row = begin + at * RUN;
+        rows = end - row;
+        at += workers;                                     // (runs and workers together stay far below 2^31)
+        return true;
+    };
+    constexpr int PER = 16 / (int)sizeof(XT), ACROSS = 64 / PER, EVERY = 32 / ACROSS;      // vectors of a row, rows at a time
+    const int wr = lane / ACROSS, wc = lane % ACROSS * PER;
+    const bool wide_in = c0 + wc < D;
+    constexpr int T_ACROSS = JT / 4, T_EVERY = 32 / T_ACROSS;
+    const int tr = lane / T_ACROSS, tc = lane % T_ACROSS * 4;
+    const bool thin_in = j0 + tc < R;
+    auto fetch = [&](int slot) {
+        int row, rows;
+        const bool some = next_run(row, rows);
+        if (some) {
+            uint8_t* w = ring + slot * Ring::STAGE;
+            const XT* src = wide + (int64_t)(row + wr) * ld + c0 + wc;
+            uint8_t* dst = w + wr * Ring::WIDE_PITCH + wc * (int)sizeof(XT);
 #pragma unroll
-            for (int st = 0; st < RUN / 8; ++st)
+            for (int k = 0; k < RUN; k += EVERY) {
+                if constexpr (VEC) {
+                    const bool there = wide_in && wr + k < rows;
+                    copy_async16(smem_u32(dst + k * Ring::WIDE_PITCH), there ? src + k * ld : wide, there);
+                } else {
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int64_t r = begin + i * RUN + st * 8 + q + 4 * h;
-#pragma unroll
-                    for (int e = 0; e < 2; ++e)
-                        load_cols<VEC>(wide + r * ld, c0 + e * 32 + g * 4, D, r < end, v[st][h][e]);
-#pragma unroll
-                    for (int n = 0; n < NT; ++n)
-                        p[st][n][h] = r < end && j0 + n * 8 + g < R ? thin[r * R + j0 + n * 8 + g] : 0.f;
-                }
-#pragma unroll
-            for (int st = 0; st < RUN / 8; ++st) {
-                float f[2][2][4];
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e)
-                        v[st][h][e].values(f[h][e]);
-#pragma unroll
-                for (int m = 0; m < 4; ++m) {              // MMA rows g and g + 8 are columns 4 g + m and 32 + 4 g + m
-                    const float w[4] = {f[0][0][m], f[0][1][m], f[1][0][m], f[1][1][m]};
-                    uint32_t wh[4], wl[4];
-                    split_four<WIDE<XT>>(w, wh, wl);
-#pragma unroll
-                    for (int n = 0; n < NT; ++n)
-                        mma_split<WIDE<XT>, true>(part[m][n], wh, wl, p[st][n][0], p[st][n][1]);
+                    for (int e = 0; e < PER; ++e)
+                        reinterpret_cast<XT*>(dst + k * Ring::WIDE_PITCH)[e] = wr + k < rows && c0 + wc + e < D ? src[k * ld + e] : from_float<XT>(0.f);
                 }
             }
-            if (++since == 4) {                            // 64 rows
-                since = 0;
+            uint8_t* t = w + RUN * Ring::WIDE_PITCH;
+            if (R % 4 == 0) {
+                const float* from = thin + (int64_t)(row + tr) * R + j0 + tc;
 #pragma unroll
-                for (int m = 0; m < 4; ++m)
-#pragma unroll
-                    for (int n = 0; n < NT; ++n)
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) {
-                            acc[m][n][k] += part[m][n][k];
-                            part[m][n][k] = 0.f;
-                        }
+                for (int k = 0; k < RUN; k += T_EVERY) {
+                    const bool there = thin_in && tr + k < rows;
+                    copy_async16(smem_u32(t + (tr + k) * Ring::THIN_PITCH + tc * 4), there ? from + k * R : thin, there);
+                }
+            } else {
+#pragma unroll 4
+                for (int i = lane; i < RUN * JT; i += 32) {
+                    const int r = i / JT, c = i % JT;
+                    const bool there = r < rows && j0 + c < R;
+                    copy_async4(smem_u32(t + r * Ring::THIN_PITCH + c * 4), there ? thin + (int64_t)(row + r) * R + j0 + c : thin, there);
+                }
             }
         }
-        runs = (int)((runs + n_runs) % workers);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        return some;
+    };
+
+    float acc[4][NT][4] = {};
+    int ahead = 0, stage = 0, put = 0;                     // runs fetched and not yet used
+#pragma unroll
+    for (int k = 0; k < STAGES - 1; ++k) {
+        ahead += fetch(put) ? 1 : 0;
+        put = put + 1 == STAGES ? 0 : put + 1;
     }
+    while (ahead > 0) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
+        __syncwarp();
+        ahead += fetch(put) ? 0 : -1;                      // into the slot that was read last, by all lanes in front of this barrier
+        put = put + 1 == STAGES ? 0 : put + 1;
+        const uint8_t* w = ring + stage * Ring::STAGE;
+        const float* t = reinterpret_cast<const float*>(w + RUN * Ring::WIDE_PITCH) + g;
+        stage = stage + 1 == STAGES ? 0 : stage + 1;
+        // MMA k: rows 2 q and 2 q + 1 (and 8 behind them); the sums of a run start from zero and are added in registers
+        if constexpr (std::is_same<XT, __nv_bfloat16>::value) {
+            // BF16 as it is, with t or u in three terms of 8 bits
+#pragma unroll
+            for (int st = 0; st < RUN / 16; ++st) {
+            uint32_t p[3][NT][2];
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    float x = t[(16 * st + 2 * q + 8 * h) * (JT + 4) + 8 * n], y = t[(16 * st + 2 * q + 1 + 8 * h) * (JT + 4) + 8 * n];
+#pragma unroll
+                    for (int e = 0; e < 3; ++e) {
+                        const __nv_bfloat162 v = __floats2bfloat162_rn(x, y);
+                        const float2 f = __bfloat1622float2(v);
+                        p[e][n][h] = *reinterpret_cast<const uint32_t*>(&v);
+                        x -= f.x;
+                        y -= f.y;
+                    }
+                }
+            uint4 v[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                v[k] = *reinterpret_cast<const uint4*>(w + (16 * st + 2 * q + (k & 1) + 8 * (k >> 1)) * Ring::WIDE_PITCH + g * 16);
+            const uint32_t* rows[4] = {&v[0].x, &v[1].x, &v[2].x, &v[3].x};
+#pragma unroll
+            for (int m0 = 0; m0 < 4; m0 += MB) {
+                float part[MB][NT][4];
+                uint32_t f[MB][4];
+#pragma unroll
+                for (int i = 0; i < MB; ++i) {             // MMA rows g and g + 8 are columns 8 g + 2 m and 8 g + 2 m + 1
+                    const int m = m0 + i;
+                    f[i][0] = __byte_perm(rows[0][m], rows[1][m], 0x5410);
+                    f[i][1] = __byte_perm(rows[0][m], rows[1][m], 0x7632);
+                    f[i][2] = __byte_perm(rows[2][m], rows[3][m], 0x5410);
+                    f[i][3] = __byte_perm(rows[2][m], rows[3][m], 0x7632);
+                }
+#pragma unroll
+                for (int e = 2; e >= 0; --e)
+#pragma unroll
+                    for (int i = 0; i < MB; ++i)
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+                            if (e == 2)
+                                mma_16_from_zero(part[i][n], f[i], p[e][n][0], p[e][n][1]);
+                            else
+                                mma_16(part[i][n], f[i], p[e][n][0], p[e][n][1], __nv_bfloat16());
+#pragma unroll
+                for (int i = 0; i < MB; ++i)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            acc[m0 + i][n][k] += part[i][n][k];
+            }
+            }
+        } else {
+#pragma unroll
+            for (int s0 = 0; s0 < RUN / 8; s0 += 2) {      // 16 rows: a sum starts from zero, and is added in registers
+                uint32_t ph[2][NT][2], pl[2][NT][2];
+                float v[2][2][8];                          // [rows 2 q, 2 q + 1][both columns of the MMA's four row tiles]
+#pragma unroll
+                for (int st = 0; st < 2; ++st)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int row = 8 * (s0 + st) + 2 * q + h;
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            const float x = t[row * (JT + 4) + 8 * n];
+                            ph[st][n][h] = high(x);
+                            pl[st][n][h] = low(x, ph[st][n][h]);
+                        }
+                        const uint8_t* r = w + row * Ring::WIDE_PITCH;
+                        if constexpr (sizeof(XT) == 4) {   // columns 4 g + m and 32 + 4 g + m
+                            const float4 x = *reinterpret_cast<const float4*>(r + g * 16), y = *reinterpret_cast<const float4*>(r + 128 + g * 16);
+                            v[st][h][0] = x.x; v[st][h][2] = x.y; v[st][h][4] = x.z; v[st][h][6] = x.w;
+                            v[st][h][1] = y.x; v[st][h][3] = y.y; v[st][h][5] = y.z; v[st][h][7] = y.w;
+                        } else {                           // columns 8 g + 2 m and 8 g + 2 m + 1
+                            Raw<XT, 8> x;
+                            const uint4 y = *reinterpret_cast<const uint4*>(r + g * 16);
+                            x.w[0] = y.x; x.w[1] = y.y; x.w[2] = y.z; x.w[3] = y.w;
+                            x.values(v[st][h]);
+                        }
+                    }
+#pragma unroll
+                for (int m0 = 0; m0 < 4; m0 += MB) {
+                    float part[MB][NT][4];
+#pragma unroll
+                    for (int st = 0; st < 2; ++st) {
+                        uint32_t wh[MB][4], wl[MB][4];
+#pragma unroll
+                        for (int i = 0; i < MB; ++i) {
+                            const int m = m0 + i;
+                            const float f[4] = {v[st][0][2 * m], v[st][0][2 * m + 1], v[st][1][2 * m], v[st][1][2 * m + 1]};
+                            split_four<WIDE<XT>>(f, wh[i], wl[i]);
+                        }
+#pragma unroll
+                        for (int e = 0; e < 3; ++e)
+#pragma unroll
+                            for (int i = 0; i < MB; ++i)
+#pragma unroll
+                                for (int n = 0; n < NT; ++n)
+                                    if (e == 0 && st == 0)
+                                        mma_tf32_from_zero(part[i][n], wh[i], pl[st][n][0], pl[st][n][1]);
+                                    else if (e == 0)
+                                        mma_tf32(part[i][n], wh[i], pl[st][n][0], pl[st][n][1]);
+                                    else if (e == 2)
+                                        mma_tf32(part[i][n], wh[i], ph[st][n][0], ph[st][n][1]);
+                                    else if (WIDE<XT>)
+                                        mma_tf32(part[i][n], wl[i], ph[st][n][0], ph[st][n][1]);
+                    }
+#pragma unroll
+                    for (int i = 0; i < MB; ++i)
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int k = 0; k < 4; ++k)
+                                acc[m0 + i][n][k] += part[i][n][k];
+                }
+            }
+        }
+    }
+    __syncthreads();                                       // the rings are free
     // parts[wk][column][rank]
 #pragma unroll
     for (int m = 0; m < 4; ++m)
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-                *reinterpret_cast<float2*>(parts + (wk * 64 + h * 32 + g * 4 + m) * RP + j0 + n * 8 + 2 * q) =
-                    make_float2(acc[m][n][2 * h] + part[m][n][2 * h], acc[m][n][2 * h + 1] + part[m][n][2 * h + 1]);
+            for (int h = 0; h < 2; ++h) {
+                const int col = sizeof(XT) == 4 ? h * 32 + g * 4 + m : g * 8 + 2 * m + h;
+                *reinterpret_cast<float2*>(parts + (wk * 64 + col) * RP + j0 + n * 8 + 2 * q) = make_float2(acc[m][n][2 * h], acc[m][n][2 * h + 1]);
+            }
     __syncthreads();
+    float* sums = a.sums + (((int64_t)blockIdx.z * a.G + id) * a.tiles + tile) * 64 * RP;
     for (int i = threadIdx.x; i < 64 * RP; i += THREADS) {
-        float v = parts[i];
-#pragma unroll
-        for (int k = 1; k < WK; ++k)
-            v += parts[k * 64 * RP + i];
-        parts[i] = v;
-    }
-    if (C > 1)
-        cluster_sync_all();
-    else
-        __syncthreads();
-    const float s = a.scale && is_b ? a.scale[id] : 1.f;
-    // every block of the cluster finishes a share; threads along the output's contiguous side
-    for (int i = (int)rank * THREADS + threadIdx.x; i < 64 * RP; i += THREADS * (int)C) {
-        const int col = is_b ? i / RP : i % 64, j = is_b ? i % RP : i / 64;
-        if (c0 + col >= D || j >= R)
-            continue;
+        int col, j;
+        tile_element(i, RP, is_b, col, j);
         float v = 0.f;
-        if (C > 1) {
-            for (uint32_t c = 0; c < C; ++c) {
-                float p;
-                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(p) : "r"(peer_smem_addr(smem_u32(parts + col * RP + j), c)));
-                v += p;
-            }
-        } else {
-            v = parts[col * RP + j];
-        }
-        if (!finite(v)) {
-            v = 0.f;
-            for (int sg = 0; sg < a.S; ++sg) {
-                if (a.ids[sg] != id)
-                    continue;
-                const int64_t begin = min(max((int64_t)a.offsets[sg], (int64_t)0), a.M), end = min(max((int64_t)a.offsets[sg + 1], (int64_t)0), a.M);
-                for (int64_t r = begin; r < end; ++r)
-                    v = fmaf(as_float(wide[r * ld + c0 + col]), thin[r * R + j], v);
-            }
-        }
-        if (is_b)
-            a.db[((int64_t)id * a.N + c0 + col) * R + j] = v * s;
-        else
-            a.da[((int64_t)id * R + j) * a.K + c0 + col] = v;
+#pragma unroll
+        for (int k = 0; k < WK; ++k)
+            v += parts[(k * 64 + col) * RP + j];
+        if (gridDim.z > 1)
+            sums[i] = v;
+        else if (c0 + col < D && j < R)
+            store_gradient<XT>(a, id, is_b, c0 + col, j, v);
     }
-    if (C > 1)
-        cluster_sync_all();
 }
 
 // ---- launches ----------------------------------------------------------------------------------------------------
@@ -767,22 +988,34 @@ cudaError_t launch_rows(const RowsArgs& a, int x_type, int w_type, cudaStream_t 
                                 : launch_rows_type<float, __half>(a, st);
 }
 
-template <typename XT, int RP, int JT, bool VEC>
-cudaError_t launch_grad_as(const GradArgs& a, int tiles, cudaStream_t st)
+int padded_rank(int R) { return R <= 16 ? 16 : R <= 32 ? 32 : R <= 64 ? 64 : 128; }
+
+int column_tiles(int64_t n) { return (int)((n + 63) / 64); }
+
+// How often the rows are split: two blocks for every SM, and 64 rows at least for a block's eight warps
+int grad_splits(int64_t M, int64_t N, int64_t K, int G)
 {
-    const size_t smem = (size_t)(WARPS / (RP / JT)) * 64 * RP * 4;
-    int c = 1;
-    while (c < 8 && (int64_t)tiles * a.G * c * 2 <= 3 * 148 && a.M > (int64_t)c * 128)
-        c *= 2;
+    const int64_t blocks = (int64_t)(column_tiles(K) + column_tiles(N)) * G, most = std::min<int64_t>(M / 64, 2 * 148 / blocks);
+    return (int)std::max<int64_t>(most, 1);
+}
+
+template <typename XT, int RP, int JT, bool VEC>
+cudaError_t launch_grad_as(const GradArgs& a, cudaStream_t st)
+{
+    using Ring = GradRing<XT, JT>;
+    const size_t smem = std::max<size_t>((size_t)(WARPS / (RP / JT)) * 64 * RP * 4, (size_t)WARPS * Ring::STAGES * Ring::STAGE);
     static std::atomic<uint64_t> known{0};
-    return launch_cluster<GradArgs>(adapter_grad_kernel<XT, RP, JT, VEC>, known, dim3((unsigned)(tiles * c), (unsigned)a.G), c, smem, st, a);
+    const cudaError_t e = launch_cluster<GradArgs>(adapter_grad_kernel<XT, RP, JT, VEC>, known, dim3(a.tiles, a.G, a.splits), 1, smem, st, a);
+    if (e != cudaSuccess || a.splits == 1)
+        return e;
+    return launch_overlapped(adapter_grad_sum_kernel<XT>, dim3(a.tiles * (64 * RP / THREADS), a.G), THREADS, 0, st, a, RP);
 }
 
 template <typename XT>
-cudaError_t launch_grad(const GradArgs& a, int tiles, cudaStream_t st)
+cudaError_t launch_grad(const GradArgs& a, cudaStream_t st)
 {
     const bool vec = vectors(a.x, a.ldx, a.K, sizeof(XT)) && vectors(a.dy, a.ld_dy, a.N, sizeof(XT));
-#define FPQ_GRAD(RP, JT) (vec ? launch_grad_as<XT, RP, JT, true>(a, tiles, st) : launch_grad_as<XT, RP, JT, false>(a, tiles, st))
+#define FPQ_GRAD(RP, JT) (vec ? launch_grad_as<XT, RP, JT, true>(a, st) : launch_grad_as<XT, RP, JT, false>(a, st))
     return a.R <= 16 ? FPQ_GRAD(16, 16) : a.R <= 32 ? FPQ_GRAD(32, 32) : a.R <= 64 ? FPQ_GRAD(64, 32) : FPQ_GRAD(128, 32);
 #undef FPQ_GRAD
 }
@@ -810,11 +1043,13 @@ cudaError_t launch_adapter_forward(const AdapterProblem& p, const void* x, int64
     return launch_rows(a, p.x_type, p.w_type, st);
 }
 
-// workspace: t [M][R] FP32, then A and B transposed
+// workspace: t [M][R] FP32, A and B transposed, the sums of the blocks that share an adapter's rows
 size_t adapter_backward_bytes(int64_t M, int64_t N, int64_t K, int G, int R, int w_type)
 {
     const size_t wb = type_bytes(w_type), g = (size_t)G * R * wb;
-    return pad16((size_t)M * R * 4) + pad16(g * K) + pad16(g * N);
+    const int splits = grad_splits(M, N, K, G);
+    const size_t sums = splits == 1 ? 0 : (size_t)splits * G * (column_tiles(K) + column_tiles(N)) * 64 * padded_rank(R) * 4;
+    return pad16((size_t)M * R * 4) + pad16(g * K) + pad16(g * N) + sums;
 }
 
 cudaError_t launch_adapter_backward(const AdapterProblem& p, const void* dy, int64_t ld_dy, const void* x, int64_t ldx, const float* u,
@@ -822,10 +1057,12 @@ cudaError_t launch_adapter_backward(const AdapterProblem& p, const void* dy, int
                                     cudaStream_t st)
 {
     float* t = (float*)workspace;
+    const size_t wb = type_bytes(p.w_type);
+    uint8_t* at = (uint8_t*)workspace + pad16((size_t)p.M * p.R * 4);
+    uint8_t* bt = at + pad16((size_t)p.G * p.R * p.K * wb);
+    float* sums = (float*)(bt + pad16((size_t)p.G * p.R * p.N * wb));
     if (p.M > 0 && p.S > 0) {
-        uint8_t* at = (uint8_t*)workspace + pad16((size_t)p.M * p.R * 4);
-        uint8_t* bt = at + pad16((size_t)p.G * p.R * p.K * type_bytes(p.w_type));
-        cudaError_t e = type_bytes(p.w_type) == 4 ? launch_transpose_as(p, (uint32_t*)at, (uint32_t*)bt, st)
+        cudaError_t e = wb == 4 ? launch_transpose_as(p, (uint32_t*)at, (uint32_t*)bt, st)
                                                   : launch_transpose_as(p, (uint16_t*)at, (uint16_t*)bt, st);
         if (e != cudaSuccess)
             return e;
@@ -841,11 +1078,11 @@ cudaError_t launch_adapter_backward(const AdapterProblem& p, const void* dy, int
     GradArgs b = {};
     b.x = x; b.dy = dy; b.t = t; b.u = u; b.scale = p.scale; b.offsets = p.offsets; b.ids = p.ids; b.da = da; b.db = db;
     b.M = p.M; b.N = p.N; b.K = p.K; b.ldx = ldx; b.ld_dy = ld_dy; b.G = p.G; b.R = p.R; b.S = p.M > 0 ? p.S : 0;
-    b.tiles_k = (int)((p.K + 63) / 64);
-    const int tiles = b.tiles_k + (int)((p.N + 63) / 64);
-    return p.x_type == FPQ_FP32   ? launch_grad<float>(b, tiles, st)
-           : p.x_type == FPQ_BF16 ? launch_grad<__nv_bfloat16>(b, tiles, st)
-                                  : launch_grad<__half>(b, tiles, st);
+    b.tiles_k = column_tiles(p.K);
+    b.tiles = b.tiles_k + column_tiles(p.N);
+    b.sums = sums;
+    b.splits = b.S > 0 ? grad_splits(p.M, p.N, p.K, p.G) : 1;
+    return p.x_type == FPQ_FP32 ? launch_grad<float>(b, st) : p.x_type == FPQ_BF16 ? launch_grad<__nv_bfloat16>(b, st) : launch_grad<__half>(b, st);
 }
 
 }  // namespace fpq
