@@ -482,7 +482,7 @@ fpq_status fpq_adapter_backward(const void* dy, int64_t ld_dy, const void* x, in
  *            number e (each tensor starts at the next multiple of 32 behind the one in front) has
  *            mix(low(e) ^ mix(t * 0x9E3779B1 + seed + 1 + high(e) * 0x243F6A89)); its upper half is m's noise, its lower
  *            half the square root's
- *   options_host  lr, weight_decay finite; beta1, beta2 in [0, 1); eps finite and not negative
+ *   options_host  lr, weight_decay finite; beta1, beta2 in [0, 1); eps zero, or a normal positive FP32 number
  *   factors  NULL (ones) or DEVICE float[2]: what a schedule or a gradient clip changes between replays of a captured call
  *   step     DEVICE int64[2] {steps made, 0}, advanced by the call; the second entry is scratch, zero before and after
  * One kernel per 400 tensors on `stream`.  Errors: FPQ_ERR_UNSUPPORTED (types), FPQ_ERR_SHAPE (count or n negative, n or

@@ -18,6 +18,9 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <math.h>
+
+#include <algorithm>
+#include <type_traits>
 #include <string.h>
 
 #include "fpq_kernels.h"
@@ -65,35 +68,99 @@ __device__ __forceinline__ float2 values_e4m3x2(uint32_t two)
     return __half22float2(v);
 }
 
-template <typename T>
-__device__ __forceinline__ float load_one(const T* p);
-template <>
-__device__ __forceinline__ float load_one<float>(const float* p) { return *p; }
-template <>
-__device__ __forceinline__ float load_one<__nv_bfloat16>(const __nv_bfloat16* p) { return __bfloat162float(*p); }
-template <>
-__device__ __forceinline__ float load_one<__half>(const __half* p) { return __half2float(*p); }
+// N values that lie side by side, as they lie, 16 (8 for four 16-bit values) bytes at a time; what they are worth is looked at where
+// they are used, so that no load waits for another
+template <int N, typename T>
+__device__ __forceinline__ void load_words(const T* p, uint32_t* w)
+{
+    if constexpr (N * sizeof(T) == 4) {
+        w[0] = *reinterpret_cast<const uint32_t*>(p);
+    } else if constexpr (N * sizeof(T) == 8) {
+        const uint2 q = *reinterpret_cast<const uint2*>(p);
+        w[0] = q.x; w[1] = q.y;
+    } else {
+#pragma unroll
+        for (int i = 0; i < N * (int)sizeof(T) / 16; ++i) {
+            const uint4 q = reinterpret_cast<const uint4*>(p)[i];
+            w[4 * i] = q.x; w[4 * i + 1] = q.y; w[4 * i + 2] = q.z; w[4 * i + 3] = q.w;
+        }
+    }
+}
 
-__device__ __forceinline__ void load_four(const float* p, float* v)
+template <typename T>
+__device__ __forceinline__ float value_at(const uint32_t* w, int i);
+template <>
+__device__ __forceinline__ float value_at<float>(const uint32_t* w, int i) { return __uint_as_float(w[i]); }
+template <>
+__device__ __forceinline__ float value_at<__nv_bfloat16>(const uint32_t* w, int i)
 {
-    const float4 q = *reinterpret_cast<const float4*>(p);
-    v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
+    return __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
 }
-__device__ __forceinline__ void load_four(const __nv_bfloat16* p, float* v)
+template <>
+__device__ __forceinline__ float value_at<__half>(const uint32_t* w, int i)
 {
-    const uint2 q = *reinterpret_cast<const uint2*>(p);
-    v[0] = __uint_as_float(q.x << 16); v[1] = __uint_as_float(q.x & 0xffff0000u);
-    v[2] = __uint_as_float(q.y << 16); v[3] = __uint_as_float(q.y & 0xffff0000u);
+    return __half2float(__ushort_as_half((unsigned short)(i & 1 ? w[i / 2] >> 16 : w[i / 2] & 0xffffu)));
 }
-__device__ __forceinline__ void load_four(const __half* p, float* v)
-{
-    const uint2 q = *reinterpret_cast<const uint2*>(p);
-    __half2 a, b;
-    memcpy(&a, &q.x, 4);
-    memcpy(&b, &q.y, 4);
-    const float2 x = __half22float2(a), y = __half22float2(b);
-    v[0] = x.x; v[1] = x.y; v[2] = y.x; v[3] = y.y;
-}
+
+// What a thread has of one run: P elements from e on, `left` of them the tensor's
+template <typename GT, bool E4>
+struct Piece {
+    static constexpr int P = E4 ? 8 : 4;
+    int64_t e;
+    int tensor, left;
+    bool fast;
+    uint32_t p[P], g[P * sizeof(GT) / 4], m[E4 ? P / 4 : P], v[E4 ? P / 4 : P], m_scale, v_scale;
+
+    template <int CAP>
+    __device__ __forceinline__ void load(const AdamwList<CAP>& L, uint32_t at)
+    {
+        using State = typename std::conditional<E4, uint8_t, float>::type;
+        int lo = 0;                        // the tensor of this run: the last one whose first run is not behind it
+        for (int hi = L.count; hi - lo > 1;) {
+            const int mid = (lo + hi) >> 1;
+            if (L.first_run[mid] <= at)
+                lo = mid;
+            else
+                hi = mid;
+        }
+        tensor = lo;
+        const fpq_adamw_tensor& T = L.t[lo];
+        e = (int64_t)(at - L.first_run[lo]) * (ADAMW_THREADS * P) + threadIdx.x * P;
+        left = e >= T.n ? 0 : T.n - e < P ? (int)(T.n - e) : P;
+        fast = left == P && L.vec[lo] != 0;
+        const State *mp = (const State*)T.m + e, *vp = (const State*)T.v + e;
+        const GT* gp = (const GT*)T.g + e;
+        if (fast) {
+            load_words<P>(T.p + e, p);
+            load_words<P>(gp, g);
+            load_words<P>(mp, m);
+            load_words<P>(vp, v);
+        } else {
+#pragma unroll
+            for (int i = 0; i < P; ++i) {
+                p[i] = i < left ? __float_as_uint(T.p[e + i]) : 0u;
+                put(g, i, i < left ? gp + i : nullptr);
+                put(m, i, i < left ? mp + i : nullptr);
+                put(v, i, i < left ? vp + i : nullptr);
+            }
+        }
+        if (E4) {
+            m_scale = left ? T.m_scale[e >> 5] : 0;
+            v_scale = left ? T.v_scale[e >> 5] : 0;
+        }
+    }
+
+    template <typename T>
+    static __device__ __forceinline__ void put(uint32_t* w, int i, const T* from)
+    {
+        constexpr int PER = 4 / (int)sizeof(T);
+        uint32_t x = 0;
+        if (from)
+            x = sizeof(T) == 4 ? *reinterpret_cast<const uint32_t*>(from)
+                : sizeof(T) == 2 ? *reinterpret_cast<const uint16_t*>(from) : *reinterpret_cast<const uint8_t*>(from);
+        w[i / PER] = (i % PER ? w[i / PER] : 0u) | x << (32 / PER * (i % PER)) % 32;
+    }
+};
 
 __device__ __forceinline__ uint32_t pack_two(float a, float b, int bf16)
 {
@@ -108,32 +175,100 @@ __device__ __forceinline__ uint32_t pack_two(float a, float b, int bf16)
     return w;
 }
 
-// magnitude bits that count towards a block's scale: infinities and NaN do not
-__device__ __forceinline__ uint32_t finite_bits(float x)
+// Four E4M3 codes of q[0 .. 3] (0 <= |q| < 256), each rounded up if the remainder below its step plus 16 bits of noise carries; noise[i]
+// holds them at bits 4 .. 19, the rest zero.  Below 2^-6 the steps are equal: with 2^-6 added they are the steps of that
+// binade.  SIGNED: with the signs, but a zero has none; otherwise what is not zero keeps the code 1 at least.
+template <bool SIGNED>
+__device__ __forceinline__ uint32_t stochastic_e4m3x4(const float* q, const uint32_t* noise)
 {
-    const uint32_t a = __float_as_uint(x) & 0x7fffffffu;
-    return a < 0x7f800000u ? a : 0u;
+    uint32_t c[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float a = SIGNED ? fabsf(q[i]) : q[i];
+        float t = a;
+        uint32_t n = noise[i] - (960u << 20);
+        if (a < 0.015625f) {
+            t = __fadd_rn(a, 0.015625f);
+            n -= 8u << 20;
+        }
+        c[i] = (__float_as_uint(t) + n) >> 20;
+        if (!SIGNED)
+            c[i] = max(c[i], min(__float_as_uint(a), 1u));
+    }
+    uint32_t w = (c[0] | c[1] << 8) | (c[2] << 16 | c[3] << 24);
+    if (SIGNED) {
+        // the top bytes of the four numbers, their signs where the code is not zero
+        const uint32_t top = __byte_perm(__byte_perm(__float_as_uint(q[0]), __float_as_uint(q[1]), 0x0073),
+                                         __byte_perm(__float_as_uint(q[2]), __float_as_uint(q[3]), 0x0073), 0x5410);
+        w |= top & (w + 0x7f7f7f7fu) & 0x80808080u;
+    }
+    return w;
 }
 
-// E4M3 code of q, |q| < 256, rounded up if the remainder below the code's step plus `noise` (16 bits) carries.  Below 2^-6 the
-// steps are equal: with 2^-6 added they are the steps of that binade.  What is not finite gets the type's NaN.
-__device__ __forceinline__ uint32_t stochastic_e4m3(float q, uint32_t noise, uint32_t least)
+// the same where some number is not finite: that one gets the type's NaN
+template <bool SIGNED>
+__device__ __noinline__ uint32_t stochastic_e4m3x4_checked(float4 q, uint4 noise)
 {
-    const float a = fabsf(q);
-    const bool low = a < 0.015625f;
-    const uint32_t word = __float_as_uint(low ? __fadd_rn(a, 0.015625f) : a) + (noise << 4);
-    uint32_t code = (word >> 20) - (low ? 968u : 960u);
-    if (a > 0.f && code < least)
-        code = least;
-    if (code)
-        code |= (__float_as_uint(q) >> 24) & 0x80u;
-    return a < 512.f ? code : 0x7fu;
+    float v[4] = {q.x, q.y, q.z, q.w};
+    const uint32_t n[4] = {noise.x, noise.y, noise.z, noise.w};
+    uint32_t bad = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if ((__float_as_uint(v[i]) & 0x7f800000u) == 0x7f800000u) {
+            bad |= 0xffu << (8 * i);
+            v[i] = 0.f;
+        }
+    return (stochastic_e4m3x4<SIGNED>(v, n) & ~bad) | (bad & 0x7f7f7f7fu);
 }
 
-// Four elements of one tensor from `e` on; g .. hold them, those from n on as zeros.
+// the largest of N numbers' finite magnitudes, as bits
+template <int N>
+__device__ __noinline__ uint32_t largest_finite(const float (&x)[N])
+{
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const uint32_t a = __float_as_uint(x[i]) & 0x7fffffffu;
+        m = max(m, a < 0x7f800000u ? a : 0u);
+    }
+    return m;
+}
+
+// 1 / d of a normal number (or infinity of zero), to a unit in the last place
+__device__ __forceinline__ float reciprocal(float d)
+{
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d));
+    return r;
+}
+
+// two numbers at a time, each operation rounded on its own
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) { return make_float2(__fmul_rn(a.x, b.x), __fmul_rn(a.y, b.y)); }
+__device__ __forceinline__ float2 add2(float2 a, float2 b) { return make_float2(__fadd_rn(a.x, b.x), __fadd_rn(a.y, b.y)); }
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) { return make_float2(__fmaf_rn(a.x, b.x, c.x), __fmaf_rn(a.y, b.y, c.y)); }
+__device__ __forceinline__ float2 both2(float v) { return make_float2(v, v); }
+__device__ __forceinline__ float2 minus(float2 v) { return make_float2(-v.x, -v.y); }
+
+// The square roots of two numbers, rounded to nearest, for v = 0 and 2^-96 <= v < infinity, without a branch: one step of
+// Goldschmidt's iteration from an approximate 1 / sqrt(v), then Markstein's correction of the result by its exact remainder
+// (P. Markstein, IBM J. Res. Dev. 34, 1990).
+__device__ __forceinline__ float2 roots_of(float2 v)
+{
+    float2 y;
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.x) : "f"(fmaxf(v.x, 1e-30f)));
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.y) : "f"(fmaxf(v.y, 1e-30f)));
+    float2 g = mul2(v, y), h = mul2(y, both2(0.5f));
+    const float2 d = fma2(minus(h), g, both2(0.5f));
+    g = fma2(g, d, g);
+    h = fma2(h, d, h);
+    return fma2(fma2(minus(g), g, v), h, g);
+}
+
 template <typename GT, bool E4, int CAP>
-__global__ void __launch_bounds__(ADAMW_THREADS) adamw_kernel(const __grid_constant__ AdamwList<CAP> L, const AdamwScalars s, int U, int bf16)
+__global__ void __launch_bounds__(ADAMW_THREADS, E4 ? 3 : 4) adamw_kernel(const __grid_constant__ AdamwList<CAP> L, const AdamwScalars s, int bf16)
 {
+    constexpr int P = Piece<GT, E4>::P;    // elements of a thread at a time
+    constexpr bool AHEAD = E4;             // the next run is fetched in front of this one's arithmetic (73.7 M elements 272 -> 255 us; FP32 moments: no gain)
     __shared__ float shared_rate, shared_root, shared_decay, shared_factor;
     __shared__ uint32_t shared_t;
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -155,120 +290,134 @@ __global__ void __launch_bounds__(ADAMW_THREADS) adamw_kernel(const __grid_const
             }
         }
     }
-    // the tensor of this run: the last one whose first run is not behind it
-    int lo = 0, hi = L.count;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (L.first_run[mid] <= blockIdx.x)
-            lo = mid;
-        else
-            hi = mid;
-    }
     __syncthreads();
     const float rate = shared_rate, root = shared_root, decay = shared_decay, factor = shared_factor;
-    if (blockIdx.x >= L.first_run[L.count])
-        return;
-    const fpq_adamw_tensor& T = L.t[lo];
-    const int64_t n = T.n, run = (int64_t)(blockIdx.x - L.first_run[lo]) * (U * ADAMW_THREADS * 4);
-    const bool vec = L.vec[lo] != 0;
-    const uint64_t number0 = L.first_block[lo] * 32u;
-
-    for (int u = 0; u < U; ++u) {
-        const int64_t e = run + (int64_t)(u * ADAMW_THREADS + threadIdx.x) * 4;
-        const int left = e >= n ? 0 : n - e < 4 ? (int)(n - e) : 4;
-        float p[4] = {}, g[4] = {}, m[4] = {}, v[4] = {};
-        uint32_t mc = 0, rc = 0;
-        const GT* gp = (const GT*)T.g + e;
-        if (left == 4 && vec) {
-            load_four(T.p + e, p);
-            load_four(gp, g);
-            if (E4) {
-                mc = *reinterpret_cast<const uint32_t*>((const uint8_t*)T.m + e);
-                rc = *reinterpret_cast<const uint32_t*>((const uint8_t*)T.v + e);
+    const bool scaled = s.factors != nullptr;
+    // (neighbouring runs at the same time: a block that took a stretch of its own was 13 % slower)
+    const uint32_t runs = L.first_run[L.count];
+    Piece<GT, E4> next;
+    if (blockIdx.x < runs)
+        next.load(L, blockIdx.x);
+    for (uint32_t at = blockIdx.x; at < runs; at += gridDim.x) {
+        const Piece<GT, E4> now = next;
+        if (AHEAD && at + gridDim.x < runs)
+            next.load(L, at + gridDim.x);
+        const fpq_adamw_tensor& T = L.t[now.tensor];
+        const int64_t e = now.e;
+        const int left = now.left;
+        float m[P], v[P], r[P], p[P];
+        bool odd_root = false;
+#pragma unroll
+        for (int i = 0; i < P; i += 2) {
+            float2 m2, v2, g2 = make_float2(value_at<GT>(now.g, i), value_at<GT>(now.g, i + 1));
+            if constexpr (E4) {
+                // a scale byte b stands for 2^(b - 127)
+                const uint32_t mb = now.m_scale, rb = now.v_scale;
+                m2 = mul2(values_e4m3x2(now.m[i / 4] >> (8 * (i % 4)) & 0xffffu), both2(__uint_as_float(mb ? mb << 23 : 0x00400000u)));
+                v2 = mul2(values_e4m3x2(now.v[i / 4] >> (8 * (i % 4)) & 0xffffu), both2(__uint_as_float(rb ? rb << 23 : 0x00400000u)));
+                v2 = mul2(v2, v2);
             } else {
-                load_four((const float*)T.m + e, m);
-                load_four((const float*)T.v + e, v);
+                m2 = make_float2(__uint_as_float(now.m[i]), __uint_as_float(now.m[i + 1]));
+                v2 = make_float2(__uint_as_float(now.v[i]), __uint_as_float(now.v[i + 1]));
             }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (i < left) {
-                    p[i] = T.p[e + i];
-                    g[i] = load_one(gp + i);
-                    if (E4) {
-                        mc |= (uint32_t)((const uint8_t*)T.m)[e + i] << (8 * i);
-                        rc |= (uint32_t)((const uint8_t*)T.v)[e + i] << (8 * i);
-                    } else {
-                        m[i] = ((const float*)T.m)[e + i];
-                        v[i] = ((const float*)T.v)[e + i];
-                    }
-                }
+            if (scaled)
+                g2 = mul2(g2, both2(factor));
+            // (each product and sum rounded on its own: 8-bit codes are then a function of the formula, not of a compiler's choice)
+            m2 = add2(mul2(m2, both2(s.beta1)), mul2(g2, both2(s.rest1)));
+            v2 = add2(mul2(v2, both2(s.beta2)), mul2(mul2(g2, g2), both2(s.rest2)));
+            const float2 r2 = roots_of(v2);
+            m[i] = m2.x; m[i + 1] = m2.y;
+            v[i] = v2.x; v[i + 1] = v2.y;
+            r[i] = r2.x; r[i + 1] = r2.y;
+            odd_root |= (v2.x < 1.2621774e-29f && v2.x > 0.f) || (v2.y < 1.2621774e-29f && v2.y > 0.f) || !(v2.x + v2.y < INFINITY);
         }
-        if (E4 && left) {
-            // a scale byte b stands for 2^(b - 127)
-            const uint32_t mb = T.m_scale[e >> 5], rb = T.v_scale[e >> 5];
-            const float ms = __uint_as_float(mb ? mb << 23 : 0x00400000u), rs = __uint_as_float(rb ? rb << 23 : 0x00400000u);
-            const float2 m0 = values_e4m3x2(mc & 0xffffu), m1 = values_e4m3x2(mc >> 16);
-            const float2 r0 = values_e4m3x2(rc & 0xffffu), r1 = values_e4m3x2(rc >> 16);
-            m[0] = m0.x * ms; m[1] = m0.y * ms; m[2] = m1.x * ms; m[3] = m1.y * ms;
-            v[0] = r0.x * rs; v[1] = r0.y * rs; v[2] = r1.x * rs; v[3] = r1.y * rs;
+        if (odd_root)                      // (2^-96, and what is not finite)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                v[i] = __fmul_rn(v[i], v[i]);
+            for (int i = 0; i < P; ++i)
+                r[i] = __fsqrt_rn(v[i]);
+#pragma unroll
+        for (int i = 0; i < P; i += 2) {
+            float2 d = fma2(make_float2(r[i], r[i + 1]), both2(root), both2(s.eps));
+            d = make_float2(reciprocal(d.x), reciprocal(d.y));
+            d = mul2(mul2(make_float2(m[i], m[i + 1]), d), both2(-rate));
+            d = fma2(make_float2(__uint_as_float(now.p[i]), __uint_as_float(now.p[i + 1])), both2(decay), d);
+            p[i] = d.x;
+            p[i + 1] = d.y;
         }
-        // (each product and sum rounded on its own: 8-bit codes are then a function of the formula, not of a compiler's choice)
-        float r[4];
+        uint32_t mc[P / 4], rc[P / 4];
+        if constexpr (E4) {
+            // the exponents of both largest magnitudes of the block, 4 threads of eight elements each
+            uint32_t a = 0, b = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float gi = s.factors ? __fmul_rn(g[i], factor) : g[i];
-            m[i] = __fadd_rn(__fmul_rn(m[i], s.beta1), __fmul_rn(gi, s.rest1));
-            v[i] = __fadd_rn(__fmul_rn(v[i], s.beta2), __fmul_rn(__fmul_rn(gi, gi), s.rest2));
-            r[i] = __fsqrt_rn(v[i]);
-            p[i] = __fsub_rn(__fmul_rn(p[i], decay), __fmul_rn(__fdividef(m[i], __fadd_rn(__fmul_rn(r[i], root), s.eps)), rate));
-        }
-        if (E4) {
-            // the exponents of both largest magnitudes of the block, 8 threads of four elements each
-            uint32_t a = max(max(finite_bits(m[0]), finite_bits(m[1])), max(finite_bits(m[2]), finite_bits(m[3]))) >> 23;
-            uint32_t b = max(max(finite_bits(r[0]), finite_bits(r[1])), max(finite_bits(r[2]), finite_bits(r[3]))) >> 23;
-            uint32_t both = left ? a << 16 | b : 0u;
-#pragma unroll
-            for (int o = 1; o < 8; o <<= 1)
-                both = __vmaxu2(both, __shfl_xor_sync(0xffffffffu, both, o));
+            for (int i = 0; i < P; ++i) {
+                a = max(a, __float_as_uint(m[i]) << 1);
+                b = max(b, __float_as_uint(r[i]));
+            }
+            const bool odd = a >= 0xff000000u || b >= 0x7f800000u;     // infinities and NaN do not count
+            if (odd) {
+                a = largest_finite<P>(m) << 1;
+                b = largest_finite<P>(r);
+            }
+            uint32_t both = (a >> 24) << 16 | b >> 23;
+            both = __vmaxu2(both, __shfl_xor_sync(0xffffffffu, both, 1));
+            both = __vmaxu2(both, __shfl_xor_sync(0xffffffffu, both, 2));
             const uint32_t mb = max((int)(both >> 16) - 7, 1), rb = max((int)(both & 0xffffu) - 7, 1);
             const float mi = __uint_as_float((254u - mb) << 23), ri = __uint_as_float((254u - rb) << 23);
-            const uint64_t number = number0 + (uint64_t)e;
+            const uint64_t number = L.first_block[now.tensor] * 32u + (uint64_t)e;
             const uint32_t key = mix(shared_t * 0x9E3779B1u + s.seed + 1u + (uint32_t)(number >> 32) * 0x243F6A89u);
-            mc = rc = 0;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t z = mix((uint32_t)(number + i) ^ key);
-                mc |= stochastic_e4m3(m[i] * mi, z >> 16, 0u) << (8 * i);
-                rc |= stochastic_e4m3(r[i] * ri, z & 0xffffu, 1u) << (8 * i);
+            for (int k = 0; k < P / 4; ++k) {
+                float qm[4], qr[4];
+                uint32_t nm[4], nr[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t z = mix((uint32_t)(number + 4 * k + i) ^ key);
+                    nm[i] = z >> 12 & 0xffff0u;
+                    nr[i] = z << 4 & 0xffff0u;
+                }
+#pragma unroll
+                for (int i = 0; i < 4; i += 2) {
+                    const float2 a2 = mul2(make_float2(m[4 * k + i], m[4 * k + i + 1]), both2(mi));
+                    const float2 b2 = mul2(make_float2(r[4 * k + i], r[4 * k + i + 1]), both2(ri));
+                    qm[i] = a2.x; qm[i + 1] = a2.y;
+                    qr[i] = b2.x; qr[i + 1] = b2.y;
+                }
+                if (!odd) {
+                    mc[k] = stochastic_e4m3x4<true>(qm, nm);
+                    rc[k] = stochastic_e4m3x4<false>(qr, nr);
+                } else {
+                    mc[k] = stochastic_e4m3x4_checked<true>(make_float4(qm[0], qm[1], qm[2], qm[3]), make_uint4(nm[0], nm[1], nm[2], nm[3]));
+                    rc[k] = stochastic_e4m3x4_checked<false>(make_float4(qr[0], qr[1], qr[2], qr[3]), make_uint4(nr[0], nr[1], nr[2], nr[3]));
+                }
             }
             if (left && (e & 31) == 0) {
                 T.m_scale[e >> 5] = (uint8_t)mb;
                 T.v_scale[e >> 5] = (uint8_t)rb;
             }
         }
-        if (left == 4 && vec) {
-            *reinterpret_cast<float4*>(T.p + e) = make_float4(p[0], p[1], p[2], p[3]);
-            if (E4) {
-                *reinterpret_cast<uint32_t*>((uint8_t*)T.m + e) = mc;
-                *reinterpret_cast<uint32_t*>((uint8_t*)T.v + e) = rc;
+        if (now.fast) {
+#pragma unroll
+            for (int i = 0; i < P; i += 4)
+                *reinterpret_cast<float4*>(T.p + e + i) = make_float4(p[i], p[i + 1], p[i + 2], p[i + 3]);
+            if constexpr (E4) {
+                *reinterpret_cast<uint2*>((uint8_t*)T.m + e) = make_uint2(mc[0], mc[1]);
+                *reinterpret_cast<uint2*>((uint8_t*)T.v + e) = make_uint2(rc[0], rc[1]);
             } else {
                 *reinterpret_cast<float4*>((float*)T.m + e) = make_float4(m[0], m[1], m[2], m[3]);
                 *reinterpret_cast<float4*>((float*)T.v + e) = make_float4(v[0], v[1], v[2], v[3]);
             }
             if (T.copy)
-                *reinterpret_cast<uint2*>((uint16_t*)T.copy + e) = make_uint2(pack_two(p[0], p[1], bf16), pack_two(p[2], p[3], bf16));
+#pragma unroll
+                for (int i = 0; i < P; i += 4)
+                    *reinterpret_cast<uint2*>((uint16_t*)T.copy + e + i) = make_uint2(pack_two(p[i], p[i + 1], bf16), pack_two(p[i + 2], p[i + 3], bf16));
         } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < P; ++i)
                 if (i < left) {
                     T.p[e + i] = p[i];
                     if (E4) {
-                        ((uint8_t*)T.m)[e + i] = (uint8_t)(mc >> (8 * i));
-                        ((uint8_t*)T.v)[e + i] = (uint8_t)(rc >> (8 * i));
+                        ((uint8_t*)T.m)[e + i] = (uint8_t)(mc[i / 4] >> (8 * (i % 4)));
+                        ((uint8_t*)T.v)[e + i] = (uint8_t)(rc[i / 4] >> (8 * (i % 4)));
                     } else {
                         ((float*)T.m)[e + i] = m[i];
                         ((float*)T.v)[e + i] = v[i];
@@ -277,13 +426,17 @@ __global__ void __launch_bounds__(ADAMW_THREADS) adamw_kernel(const __grid_const
                         ((uint16_t*)T.copy)[e + i] = (uint16_t)pack_two(p[i], 0.f, bf16);
                 }
         }
+        if (!AHEAD && at + gridDim.x < runs)
+            next.load(L, at + gridDim.x);
     }
 }
 
 template <int CAP>
-cudaError_t launch_list(const AdamwList<CAP>& L, const AdamwScalars& s, int g_type, int bf16, int e4, int U, cudaStream_t st)
+cudaError_t launch_list(const AdamwList<CAP>& L, const AdamwScalars& s, int g_type, int bf16, int e4, cudaStream_t st)
 {
-    const dim3 grid(L.first_run[L.count] ? L.first_run[L.count] : 1);
+    // as many blocks as an SM holds, which go from run to run
+    uint32_t most = 148 * (e4 ? 3 : 4);
+    const dim3 grid(std::min(std::max(L.first_run[L.count], 1u), most));
     // (as launch_overlapped, but the list is not copied on its way)
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
@@ -294,7 +447,7 @@ cudaError_t launch_list(const AdamwList<CAP>& L, const AdamwScalars& s, int g_ty
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    void* args[] = {(void*)&L, (void*)&s, &U, &bf16};
+    void* args[] = {(void*)&L, (void*)&s, &bf16};
 #define FPQ_ADAMW(GT) cudaLaunchKernelExC(&cfg, e4 ? (const void*)adamw_kernel<GT, true, CAP> : (const void*)adamw_kernel<GT, false, CAP>, args)
     return g_type == FPQ_FP32 ? FPQ_ADAMW(float) : g_type == FPQ_BF16 ? FPQ_ADAMW(__nv_bfloat16) : FPQ_ADAMW(__half);
 #undef FPQ_ADAMW
@@ -302,15 +455,15 @@ cudaError_t launch_list(const AdamwList<CAP>& L, const AdamwScalars& s, int g_ty
 
 bool vectors(const fpq_adamw_tensor& t, int g_type, int e4)
 {
-    const uintptr_t g = g_type == FPQ_FP32 ? 16 : 8, state = e4 ? 4 : 16;
+    const uintptr_t g = g_type == FPQ_FP32 || e4 ? 16 : 8, state = e4 ? 8 : 16;
     return (uintptr_t)t.p % 16 == 0 && (uintptr_t)t.g % g == 0 && (uintptr_t)t.m % state == 0 && (uintptr_t)t.v % state == 0 &&
            (uintptr_t)t.copy % 8 == 0;
 }
 
 template <int CAP>
-fpq_status launch_all(const fpq_adamw_tensor* t, int count, AdamwScalars s, int g_type, int bf16, int e4, int U, cudaStream_t st)
+fpq_status launch_all(const fpq_adamw_tensor* t, int count, AdamwScalars s, int g_type, int bf16, int e4, cudaStream_t st)
 {
-    const int64_t run = (int64_t)U * ADAMW_THREADS * 4;
+    const int64_t run = ADAMW_THREADS * (e4 ? 8 : 4);
     uint64_t block = 0;
     int at = 0;
     do {
@@ -321,8 +474,8 @@ fpq_status launch_all(const fpq_adamw_tensor* t, int count, AdamwScalars s, int 
             if (t[at].n == 0)
                 continue;
             const int64_t more = (t[at].n + run - 1) / run;
-            if (runs + more > 0x7fffffff)
-                break;                     // (never the first of a launch: n < 2^40)
+            if (runs + more > 0x7fffffff && k > 0)
+                break;
             L.t[k] = t[at];
             L.first_run[k] = runs;
             L.first_block[k] = block;
@@ -334,7 +487,7 @@ fpq_status launch_all(const fpq_adamw_tensor* t, int count, AdamwScalars s, int 
         L.first_run[k] = runs;
         L.count = k;
         s.last = at == count;
-        if (launch_list(L, s, g_type, bf16, e4, U, st) != cudaSuccess)
+        if (launch_list(L, s, g_type, bf16, e4, st) != cudaSuccess)
             return FPQ_ERR_CUDA;
     } while (at < count);
     return FPQ_OK;
@@ -359,14 +512,9 @@ fpq_status launch_adamw(const fpq_adamw_tensor* t, int count, int g_type, int co
     s.factors = factors;
     s.step = (long long*)step;
     s.last = 0;
-    int64_t total = 0;
-    for (int i = 0; i < count; ++i)
-        total += t[i].n;
-    // runs of 1024 elements spread small calls over the SMs, runs of 4096 spend less on finding their tensor
-    const int U = total >= (int64_t)148 * 8 * 4096 ? 4 : 1;
     const int bf16 = copy_type == FPQ_BF16, e4 = state_type == FPQ_E4M3_BLOCK32;
-    return count <= ADAMW_SMALL ? launch_all<ADAMW_SMALL>(t, count, s, g_type, bf16, e4, U, st)
-                                : launch_all<ADAMW_LAUNCH>(t, count, s, g_type, bf16, e4, U, st);
+    return count <= ADAMW_SMALL ? launch_all<ADAMW_SMALL>(t, count, s, g_type, bf16, e4, st)
+                                : launch_all<ADAMW_LAUNCH>(t, count, s, g_type, bf16, e4, st);
 }
 
 }  // namespace fpq

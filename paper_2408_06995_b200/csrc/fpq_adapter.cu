@@ -256,16 +256,57 @@ struct RowsArgs {
     int wr;                        // row groups of a block: 1, 2, 4 or 8
 };
 
+__device__ __forceinline__ void copy_async16(uint32_t dst, const void* src, bool there)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+}
+__device__ __forceinline__ void copy_async4(uint32_t dst, const void* src, bool there)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(there ? 4 : 0) : "memory");
+}
+
+// A warp's share of 32 columns of a row: for FP32 rows, columns 4 q .. and 16 + 4 q .. (q = lane % 4), for 16-bit rows 8 q ..: a vector per
+// lane, the vectors of a row side by side.
+template <typename XT>
+__device__ __forceinline__ int group_column(int q, int i) { return sizeof(XT) == 4 ? (i >> 2) * 16 + 4 * q + (i & 3) : 8 * q + i; }
+
+template <typename XT, bool VEC, typename T>
+__device__ __forceinline__ void load_group(const T* row, int c0, int q, int width, bool there, Raw<T, 8>& r)
+{
+    if constexpr (sizeof(XT) == 4) {
+        Raw<T, 4> a, b;
+        load_cols<VEC>(row, c0 + 4 * q, width, there, a);
+        load_cols<VEC>(row, c0 + 16 + 4 * q, width, there, b);
+#pragma unroll
+        for (int i = 0; i < Raw<T, 4>::WORDS; ++i) {
+            r.w[i] = a.w[i];
+            r.w[Raw<T, 4>::WORDS + i] = b.w[i];
+        }
+    } else {
+        load_cols<VEC>(row, c0 + 8 * q, width, there, r);
+    }
+}
+
+// Every warp has a ring of its own in shared memory through which its 16 rows of x come, and behind them those of base, in groups of
+// 32 columns: fetched asynchronously STAGES - 1 groups ahead, no warp waits for another.
+template <typename XT, int RP>
+struct RowsRing {
+    static constexpr int SLOT = 16 * 32 * (int)sizeof(XT);
+    static constexpr int STAGES = sizeof(XT) == 2 ? (RP <= 32 ? 8 : 4) : RP <= 32 ? 4 : RP == 64 ? 2 : 4;   // two blocks on an SM up to rank 64
+};
+
 // A block has 16 * wr rows; each of its warps takes 16 of them and, with the 8 / wr warps (times the blocks of the cluster) that
 // have the same rows, shares the reduction in groups of 32 columns, then the output in groups of 32 columns.  RP: the rank, padded.
 template <typename XT, typename WT, int RP, bool VEC>
 __global__ void __launch_bounds__(THREADS, RP <= 64 ? 2 : 1) adapter_rows_kernel(const RowsArgs a)
 {
-    constexpr int NT = RP / 8, PITCH = RP == 16 ? 16 : RP + 16;
+    using Ring = RowsRing<XT, RP>;
+    constexpr int NT = RP / 8, PITCH = RP == 16 ? 16 : RP + 16, STAGES = Ring::STAGES;
     constexpr bool NATIVE = sizeof(XT) == 2;               // x and weights of one 16-bit type, multiplied as they are
-    constexpr bool AHEAD = RP <= 16;                       // registers for the weights of the next group
+    constexpr bool AHEAD = RP * sizeof(WT) <= 64;          // registers for the weights of the next group
     extern __shared__ float4 smem4[];
-    float* parts = reinterpret_cast<float*>(smem4);        // [8 / wr][16 wr][RP], then the block's sum in the first
+    uint8_t* rings = reinterpret_cast<uint8_t*>(smem4);
+    float* parts = reinterpret_cast<float*>(rings + WARPS * STAGES * Ring::SLOT);   // [8 / wr][16 wr][RP], then the block's sum in the first
     float* t_smem = parts + WARPS * 16 * RP;               // [16 wr][PITCH]
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -278,84 +319,127 @@ __global__ void __launch_bounds__(THREADS, RP <= 64 ? 2 : 1) adapter_rows_kernel
     if (tr.rows <= 0)
         return;                                            // (every block of the cluster leaves)
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
-    const int r0 = (warp & (WR - 1)) * 16, wk = warp / WR;
+    const int r0 = (warp & (WR - 1)) * 16, wk = warp / WR, here = tr.rows - r0;
     const float s = a.scale && tr.id >= 0 ? a.scale[tr.id] : 1.f;
     const int D1 = (int)a.D1, D2 = (int)a.D2, R = a.R, step = 32 * WK * (int)C, first = 32 * ((int)rank * WK + wk);
+    const WT* w1 = (const WT*)a.w1 + (int64_t)max(tr.id, 0) * R * D1;
     const WT* w2 = (const WT*)a.w2 + (int64_t)max(tr.id, 0) * R * D2;
-    const bool there[2] = {r0 + g < tr.rows, r0 + 8 + g < tr.rows};
+    const XT* in = (const XT*)a.in + tr.row * a.ld_in;
+
+    // what comes through the ring: groups of x, then groups of base
+    uint8_t* ring = rings + warp * (STAGES * Ring::SLOT);
+    constexpr int PER = 16 / (int)sizeof(XT), ACROSS = 32 / PER, EVERY = 32 / ACROSS;       // values of a vector, vectors of a row, rows at a time
+    const int cr = lane / ACROSS, cc = lane % ACROSS;
+    const int xs = here > 0 && tr.id >= 0 && first < D1 ? (D1 - 1 - first) / step + 1 : 0;
+    const int bs = here > 0 && a.out && a.base && first < D2 ? (D2 - 1 - first) / step + 1 : 0;
+    const XT* x_from = in + (int64_t)(r0 + cr) * a.ld_in + first + cc * PER;
+    const XT* b_from = (const XT*)a.base + (tr.row + r0 + cr) * a.ld_base + first + cc * PER;
+    int fetched = 0, put = 0, get = 0;
+    auto fetch = [&]() {
+        if (fetched < xs + bs) {
+            const bool is_x = fetched < xs;
+            const int i = is_x ? fetched : fetched - xs, col = first + i * step + cc * PER, width = is_x ? D1 : D2;
+            const int64_t ld = is_x ? a.ld_in : a.ld_base;
+            const XT* src = (is_x ? x_from : b_from) + (int64_t)i * step;
+            uint8_t* slot = ring + put * Ring::SLOT;
+#pragma unroll
+            for (int k = 0; k < 16; k += EVERY) {
+                // FP32: eight vectors a row; the halves of odd rows are exchanged, so that two rows' vectors lie in different banks
+                const int r = cr + k, c = sizeof(XT) == 4 ? cc ^ ((r & 1) << 2) : cc;
+                uint8_t* dst = slot + r * (32 * (int)sizeof(XT)) + c * 16;
+                if constexpr (VEC) {
+                    const bool there = r < here && col < width;
+                    copy_async16(smem_u32(dst), there ? src + k * ld : in, there);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < PER; ++e)
+                        reinterpret_cast<XT*>(dst)[e] = r < here && col + e < width ? src[k * ld + e] : from_float<XT>(0.f);
+                }
+            }
+        }
+        ++fetched;
+        put = put + 1 == STAGES ? 0 : put + 1;
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    auto take = [&](Raw<XT, 8> (&v)[2]) {                  // the next group of rows g and g + 8
+        asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 2) : "memory");
+        __syncwarp();
+        fetch();                                           // into the slot that was read last, by all lanes in front of this barrier
+        const uint8_t* slot = ring + get * Ring::SLOT;
+        get = get + 1 == STAGES ? 0 : get + 1;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const uint8_t* row = slot + (g + 8 * h) * (32 * (int)sizeof(XT));
+#pragma unroll
+            for (int e = 0; e < (int)sizeof(XT) / 2; ++e) {
+                const uint4 x = *reinterpret_cast<const uint4*>(row + (sizeof(XT) == 4 ? ((q + 4 * e) ^ ((g & 1) << 2)) * 16 : q * 16));
+                v[h].w[4 * e] = x.x; v[h].w[4 * e + 1] = x.y; v[h].w[4 * e + 2] = x.z; v[h].w[4 * e + 3] = x.w;
+            }
+        }
+    };
+#pragma unroll
+    for (int k = 0; k < STAGES - 1; ++k)
+        fetch();
 
     if (tr.id >= 0) {
-        const XT* in = (const XT*)a.in + tr.row * a.ld_in;
-        const WT* w1 = (const WT*)a.w1 + (int64_t)tr.id * R * D1;
-        const XT* x_row[2] = {in + (r0 + g) * a.ld_in, in + (r0 + 8 + g) * a.ld_in};
         float acc[NT][4] = {}, part[NT][4] = {};
-        Raw<XT, 8> x[2], x_next[2];
+        Raw<XT, 8> x[2];
         Raw<WT, 8> w[NT], w_next[AHEAD ? NT : 1];
+        const WT* w_row = w1 + (int64_t)g * D1;
         int since = 0;
-        if (r0 < tr.rows && first < D1) {
+        if (AHEAD && xs > 0)
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-                load_cols<VEC>(x_row[h], first + q * 8, D1, there[h], x_next[h]);
-            if (AHEAD)
+            for (int n = 0; n < NT; ++n)
+                load_group<XT, VEC>(w_row + (int64_t)(n * 8) * D1, first, q, D1, n * 8 + g < R, w_next[n]);
+        for (int i = 0; i < xs; ++i) {
+            const int k0 = first + i * step;
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
-                    load_cols<VEC>(w1 + (int64_t)(n * 8 + g) * D1, first + q * 8, D1, n * 8 + g < R, w_next[n]);
-            for (int k0 = first; k0 < D1; k0 += step) {
-                x[0] = x_next[0];
-                x[1] = x_next[1];
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-                    if (AHEAD)
-                        w[n] = w_next[n];
-                    else
-                        load_cols<VEC>(w1 + (int64_t)(n * 8 + g) * D1, k0 + q * 8, D1, n * 8 + g < R, w[n]);
-                const int k1 = k0 + step + q * 8;          // (behind the end nothing is loaded)
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-                    load_cols<VEC>(x_row[h], k1, D1, there[h], x_next[h]);
-                if (AHEAD)
-#pragma unroll
-                    for (int n = 0; n < NT; ++n)
-                        load_cols<VEC>(w1 + (int64_t)(n * 8 + g) * D1, k1, D1, n * 8 + g < R, w_next[n]);
-                if constexpr (NATIVE) {
-#pragma unroll
-                    for (int st = 0; st < 2; ++st) {
-                        const uint32_t v[4] = {x[0].w[2 * st], x[1].w[2 * st], x[0].w[2 * st + 1], x[1].w[2 * st + 1]};
-#pragma unroll
-                        for (int n = 0; n < NT; ++n)
-                            mma_16(part[n], v, w[n].w[2 * st], w[n].w[2 * st + 1], XT());
-                    }
+            for (int n = 0; n < NT; ++n)
+                if (AHEAD) {
+                    w[n] = w_next[n];
+                    load_group<XT, VEC>(w_row + (int64_t)(n * 8) * D1, k0 + step, q, D1, n * 8 + g < R, w_next[n]);   // (behind the end nothing is loaded)
                 } else {
-                    float f[2][8], fw[NT][8];
-                    x[0].values(f[0]);
-                    x[1].values(f[1]);
+                    load_group<XT, VEC>(w_row + (int64_t)(n * 8) * D1, k0, q, D1, n * 8 + g < R, w[n]);
+                }
+            take(x);
+            if constexpr (NATIVE) {
+#pragma unroll
+                for (int st = 0; st < 2; ++st) {
+                    const uint32_t v[4] = {x[0].w[2 * st], x[1].w[2 * st], x[0].w[2 * st + 1], x[1].w[2 * st + 1]};
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
-                        w[n].values(fw[n]);
+                        mma_16(part[n], v, w[n].w[2 * st], w[n].w[2 * st + 1], XT());
+                }
+            } else {
+                float f[2][8], fw[NT][8];
+                x[0].values(f[0]);
+                x[1].values(f[1]);
 #pragma unroll
-                    for (int st = 0; st < 4; ++st) {
-                        const float v[4] = {f[0][2 * st], f[1][2 * st], f[0][2 * st + 1], f[1][2 * st + 1]};
-                        uint32_t vh[4], vl[4];
-                        split_four<true>(v, vh, vl);
-                        float b[NT][2];
+                for (int n = 0; n < NT; ++n)
+                    w[n].values(fw[n]);
 #pragma unroll
-                        for (int n = 0; n < NT; ++n) {
-                            b[n][0] = fw[n][2 * st];
-                            b[n][1] = fw[n][2 * st + 1];
-                        }
-                        mma_split<true, WIDE<WT>, NT>(part, vh, vl, b);
+                for (int st = 0; st < 4; ++st) {
+                    const float v[4] = {f[0][2 * st], f[1][2 * st], f[0][2 * st + 1], f[1][2 * st + 1]};
+                    uint32_t vh[4], vl[4];
+                    split_four<true>(v, vh, vl);
+                    float b[NT][2];
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        b[n][0] = fw[n][2 * st];
+                        b[n][1] = fw[n][2 * st + 1];
                     }
+                    mma_split<true, WIDE<WT>, NT>(part, vh, vl, b);
                 }
-                if (++since == 2) {                        // 64 columns
-                    since = 0;
+            }
+            if (++since == 2) {                            // 64 columns
+                since = 0;
 #pragma unroll
-                    for (int n = 0; n < NT; ++n)
+                for (int n = 0; n < NT; ++n)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            acc[n][i] += part[n][i];
-                            part[n][i] = 0.f;
-                        }
-                }
+                    for (int k = 0; k < 4; ++k) {
+                        acc[n][k] += part[n][k];
+                        part[n][k] = 0.f;
+                    }
             }
         }
         float* mine = parts + (wk * BM + r0) * RP;
@@ -404,32 +488,31 @@ __global__ void __launch_bounds__(THREADS, RP <= 64 ? 2 : 1) adapter_rows_kernel
             a.kept[tr.row * R + i] = 0.f;
     }
 
-    if (a.out && r0 < tr.rows) {
-        // BF16: t in two terms of 8 bits, 2^-17 of it left out against the 2^-9 that y is rounded by; otherwise TF32 terms
+    if (a.out && here > 0) {
+        // BF16: t in two terms of 8 bits, 2^-18 of it left out against the 2^-9 that y is rounded by; otherwise TF32 terms
         constexpr bool BF = std::is_same<XT, __nv_bfloat16>::value;
-        constexpr int PER = RP < 32 ? RP / 4 : 8, BLOCKS = RP / (4 * PER);   // ranks of a thread side by side, and how often
-        constexpr bool HOLD = BF || RP <= 32;                                // t's operands stay in registers
-        const XT* base = (const XT*)a.base + tr.row * a.ld_base;
-        XT* out = (XT*)a.out + tr.row * a.ld_out;
-        uint32_t th[HOLD ? BLOCKS : 1][PER / 2][4], tl[HOLD ? BLOCKS : 1][PER / 2][4];
-        auto fetch_t = [&](int b, uint32_t (&h)[PER / 2][4], uint32_t (&l)[PER / 2][4]) {
-            float t[2][PER];
+        constexpr int TPER = RP < 32 ? RP / 4 : 8, BLOCKS = RP / (4 * TPER);  // ranks of a thread side by side, and how often
+        constexpr bool HOLD = BF || RP <= 32;                                 // t's operands stay in registers
+        constexpr bool AHEAD2 = RP * sizeof(WT) <= 64;
+        uint32_t th[HOLD ? BLOCKS : 1][TPER / 2][4], tl[HOLD ? BLOCKS : 1][TPER / 2][4];
+        auto fetch_t = [&](int b, uint32_t (&h)[TPER / 2][4], uint32_t (&l)[TPER / 2][4]) {
+            float t[2][TPER];
 #pragma unroll
             for (int k = 0; k < 2; ++k)
 #pragma unroll
-                for (int i = 0; i < PER; i += 4) {
-                    const float4 v = *reinterpret_cast<const float4*>(t_smem + (r0 + k * 8 + g) * PITCH + (b * 4 + q) * PER + i);
+                for (int i = 0; i < TPER; i += 4) {
+                    const float4 v = *reinterpret_cast<const float4*>(t_smem + (r0 + k * 8 + g) * PITCH + (b * 4 + q) * TPER + i);
                     t[k][i] = v.x; t[k][i + 1] = v.y; t[k][i + 2] = v.z; t[k][i + 3] = v.w;
                 }
             if constexpr (BF) {
 #pragma unroll
-                for (int st = 0; st < PER / 4; ++st)
+                for (int st = 0; st < TPER / 4; ++st)
 #pragma unroll
                     for (int e = 0; e < 4; ++e)            // rows g, g + 8, then the second pair of ranks
                         split_bf16(t[e & 1][4 * st + 2 * (e >> 1)], t[e & 1][4 * st + 2 * (e >> 1) + 1], h[st][e], l[st][e]);
             } else {
 #pragma unroll
-                for (int st = 0; st < PER / 2; ++st) {
+                for (int st = 0; st < TPER / 2; ++st) {
                     const float v[4] = {t[0][2 * st], t[1][2 * st], t[0][2 * st + 1], t[1][2 * st + 1]};
                     split_four<true>(v, h[st], l[st]);
                 }
@@ -440,98 +523,115 @@ __global__ void __launch_bounds__(THREADS, RP <= 64 ? 2 : 1) adapter_rows_kernel
 #pragma unroll
                 for (int b = 0; b < BLOCKS; ++b)
                     fetch_t(b, th[b], tl[b]);
-        Raw<XT, 8> y0[2];
-        const bool based = a.base != nullptr;
+        // The MMA's column g of tile e is this output column: the two columns 2 q and 2 q + 1 that a thread gets of each of the four
+        // tiles are its columns of the group.
+        const int n0 = sizeof(XT) == 4 ? 4 * (g >> 1) + (g & 1) : 8 * (g >> 1) + (g & 1);
+        auto tile_column = [](int e) { return sizeof(XT) == 4 ? (e >> 1) * 16 + (e & 1) * 2 : 2 * e; };
+        auto load_w2 = [&](int c0, int b, Raw<WT, TPER> (&w)[4]) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-            load_cols<VEC>(base + (r0 + h * 8 + g) * a.ld_base, first + q * 8, D2, based && there[h], y0[h]);
+            for (int e = 0; e < 4; ++e) {
+                const int n = c0 + n0 + tile_column(e);
+                load_cols<VEC>(w2 + (int64_t)n * R, (b * 4 + q) * TPER, R, n < D2, w[e]);
+            }
+        };
+        Raw<WT, TPER> w_next[AHEAD2 ? BLOCKS : 1][4];
+        if (AHEAD2 && tr.id >= 0)
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b)
+                load_w2(first, b, w_next[AHEAD2 ? b : 0]);
+        XT* out_row[2] = {(XT*)a.out + (tr.row + r0 + g) * a.ld_out, (XT*)a.out + (tr.row + r0 + 8 + g) * a.ld_out};
         for (int c0 = first; c0 < D2; c0 += step) {
-            const int col = c0 + q * 8;                    // this thread's 8 columns of rows g and g + 8
             float y[2][8], acc[4][4] = {};
             if (tr.id >= 0) {
-                // output column of the MMA's column g in tile e: the two columns 2 q and 2 q + 1 that a thread gets of each
-                // of the four tiles are its 8 columns
-                const int n = c0 + 8 * (g >> 1) + (g & 1);
 #pragma unroll
                 for (int b = 0; b < BLOCKS; ++b) {
-                    Raw<WT, PER> w[4];
+                    Raw<WT, TPER> w[4];
+                    if constexpr (AHEAD2) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        load_cols<VEC>(w2 + (int64_t)(n + 2 * e) * R, (b * 4 + q) * PER, R, n + 2 * e < D2, w[e]);
+                        for (int e = 0; e < 4; ++e)
+                            w[e] = w_next[b][e];
+                        load_w2(c0 + step, b, w_next[b]);
+                    } else {
+                        load_w2(c0, b, w);
+                    }
                     if constexpr (!HOLD)
                         fetch_t(b, th[0], tl[0]);
                     const auto& h = th[HOLD ? b : 0];
                     const auto& l = tl[HOLD ? b : 0];
                     if constexpr (BF) {
 #pragma unroll
-                        for (int st = 0; st < PER / 4; ++st)
+                        for (int st = 0; st < TPER / 4; ++st)
+#pragma unroll
                             for (int k = 0; k < 2; ++k)
 #pragma unroll
                                 for (int e = 0; e < 4; ++e)
                                     mma_16(acc[e], k ? h[st] : l[st], w[e].w[2 * st], w[e].w[2 * st + 1], __nv_bfloat16());
                     } else {
-                        float f[4][PER];
+                        float f[4][TPER];
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
                             w[e].values(f[e]);
 #pragma unroll
-                        for (int st = 0; st < PER / 2; ++st) {
+                        for (int st = 0; st < TPER / 2; ++st) {
                             const float v[4][2] = {{f[0][2 * st], f[0][2 * st + 1]}, {f[1][2 * st], f[1][2 * st + 1]},
                                                    {f[2][2 * st], f[2][2 * st + 1]}, {f[3][2 * st], f[3][2 * st + 1]}};
                             mma_split<true, WIDE<WT>, 4>(acc, h[st], l[st], v);
                         }
                     }
                 }
-            }
+                float zero = 0.f;                          // becomes NaN if a sum is not finite
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                y0[h].values(y[h]);
-                load_cols<VEC>(base + (r0 + h * 8 + g) * a.ld_base, col + step, D2, based && there[h], y0[h]);
-            }
-            bool odd = false;
+                for (int e = 0; e < 4; ++e)
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+                    for (int k = 0; k < 4; ++k)
+                        zero = fmaf(acc[e][k], 0.f, zero);
+                if (zero != 0.f) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    odd |= !finite(acc[i >> 1][2 * h + (i & 1)]);
-                }
-            if (odd)
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        float& v = acc[i >> 1][2 * h + (i & 1)];
-                        const int r = r0 + h * 8 + g;
-                        if (!finite(v) && r < tr.rows && col + i < D2) {
+                    for (int i = 0; i < 16; ++i) {
+                        const int h = i >> 3, r = r0 + h * 8 + g, col = c0 + group_column<XT>(q, i & 7);
+                        float& v = acc[(i & 7) >> 1][2 * h + (i & 1)];
+                        if (!finite(v) && r < tr.rows && col < D2) {
                             v = 0.f;
                             for (int j = 0; j < R; ++j)
-                                v = fmaf(t_smem[r * PITCH + j], as_float(w2[(int64_t)(col + i) * R + j]), v);
+                                v = fmaf(t_smem[r * PITCH + j], as_float(w2[(int64_t)col * R + j]), v);
                         }
                     }
+                }
+            }
+            if (bs > 0) {
+                Raw<XT, 8> y0[2];
+                take(y0);
+                y0[0].values(y[0]);
+                y0[1].values(y[1]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    y[i >> 3][i & 7] = 0.f;
+            }
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
                     y[h][i] += acc[i >> 1][2 * h + (i & 1)];
-                if (!there[h])
+                if (8 * h + g >= here)
                     continue;
-                XT* o = out + (r0 + h * 8 + g) * a.ld_out + col;
-                constexpr int PIECE = 16 / (int)sizeof(XT);
+                XT* o = out_row[h] + c0;
 #pragma unroll
-                for (int p = 0; p < 8; p += PIECE) {
+                for (int p = 0; p < 8; p += PER) {
+                    const int col = group_column<XT>(q, p);
                     if (VEC) {
-                        if (col + p < D2) {
-                            alignas(16) XT v[PIECE];
+                        if (c0 + col < D2) {
+                            alignas(16) XT v[PER];
 #pragma unroll
-                            for (int i = 0; i < PIECE; ++i)
+                            for (int i = 0; i < PER; ++i)
                                 v[i] = from_float<XT>(y[h][p + i]);
-                            *reinterpret_cast<uint4*>(o + p) = *reinterpret_cast<const uint4*>(v);
+                            *reinterpret_cast<uint4*>(o + col) = *reinterpret_cast<const uint4*>(v);
                         }
                     } else {
 #pragma unroll
-                        for (int i = 0; i < PIECE; ++i)
-                            if (col + p + i < D2)
-                                o[p + i] = from_float<XT>(y[h][p + i]);
+                        for (int i = 0; i < PER; ++i)
+                            if (c0 + col + i < D2)
+                                o[col + i] = from_float<XT>(y[h][p + i]);
                     }
                 }
             }
@@ -631,15 +731,6 @@ __global__ void __launch_bounds__(THREADS) adapter_grad_sum_kernel(const GradArg
     for (int z = 0; z < a.splits; ++z)
         v += s[z * step];
     store_gradient<XT>(a, id, is_b, col, j, v);
-}
-
-__device__ __forceinline__ void copy_async16(uint32_t dst, const void* src, bool there)
-{
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void copy_async4(uint32_t dst, const void* src, bool there)
-{
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(there ? 4 : 0) : "memory");
 }
 
 // Every warp has a ring of its own in shared memory: runs of 16 (32) rows of 64 columns and of its JT ranks, fetched
@@ -905,16 +996,16 @@ __global__ void __launch_bounds__(THREADS, 2) adapter_grad_kernel(const GradArgs
 
 // ---- launches ----------------------------------------------------------------------------------------------------
 template <typename Args>
-cudaError_t launch_cluster(void (*kernel)(const Args), std::atomic<uint64_t>& known, dim3 grid, int cluster, size_t smem, cudaStream_t st,
-                           const Args& args)
+cudaError_t launch_cluster(void (*kernel)(const Args), std::atomic<uint64_t>& known, int most, dim3 grid, int cluster, size_t smem,
+                           cudaStream_t st, const Args& args)
 {
-    // shared memory beyond 48 KB is asked for once per kernel and device
+    // shared memory beyond 48 KB is asked for once per kernel and device: `most`, what any call of this kernel needs
     int dev = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess)
         return e;
-    if (smem > 48 * 1024 && (dev >= 64 || !(known.load(std::memory_order_relaxed) >> dev & 1))) {
-        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (most > 48 * 1024 && (dev >= 64 || !(known.load(std::memory_order_relaxed) >> dev & 1))) {
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
         if (e != cudaSuccess)
             return e;
         if (dev < 64)
@@ -954,7 +1045,7 @@ cudaError_t launch_rows_as(RowsArgs a, cudaStream_t st)
     while (a.wr < 8 && a.M / (16 * a.wr) + a.S > 2 * 148 && a.M >= 24 * a.wr * (int64_t)a.S)
         a.wr *= 2;
     const int BM = 16 * a.wr;
-    const size_t smem = (size_t)(WARPS * 16 * RP + BM * PITCH) * 4;
+    const size_t smem = (size_t)WARPS * RowsRing<XT, RP>::STAGES * RowsRing<XT, RP>::SLOT + (size_t)(WARPS * 16 * RP + BM * PITCH) * 4;
     const int64_t tiles = a.M / BM + a.S;
     // clusters until there are two blocks for every SM, while every block has a group of columns for most of its warps
     int c = 1;
@@ -962,7 +1053,8 @@ cudaError_t launch_rows_as(RowsArgs a, cudaStream_t st)
     while (c < 8 && busy * c * 2 <= 2 * 148 && groups > (int64_t)c * (WARPS / a.wr))
         c *= 2;
     static std::atomic<uint64_t> known{0};
-    return launch_cluster<RowsArgs>(adapter_rows_kernel<XT, WT, RP, VEC>, known, dim3((unsigned)(tiles * c)), c, smem, st, a);
+    constexpr int MOST = WARPS * RowsRing<XT, RP>::STAGES * RowsRing<XT, RP>::SLOT + (WARPS * 16 * RP + 16 * WARPS * PITCH) * 4;
+    return launch_cluster<RowsArgs>(adapter_rows_kernel<XT, WT, RP, VEC>, known, MOST, dim3((unsigned)(tiles * c)), c, smem, st, a);
 }
 
 template <typename XT, typename WT>
@@ -1005,7 +1097,7 @@ cudaError_t launch_grad_as(const GradArgs& a, cudaStream_t st)
     using Ring = GradRing<XT, JT>;
     const size_t smem = std::max<size_t>((size_t)(WARPS / (RP / JT)) * 64 * RP * 4, (size_t)WARPS * Ring::STAGES * Ring::STAGE);
     static std::atomic<uint64_t> known{0};
-    const cudaError_t e = launch_cluster<GradArgs>(adapter_grad_kernel<XT, RP, JT, VEC>, known, dim3(a.tiles, a.G, a.splits), 1, smem, st, a);
+    const cudaError_t e = launch_cluster<GradArgs>(adapter_grad_kernel<XT, RP, JT, VEC>, known, (int)smem, dim3(a.tiles, a.G, a.splits), 1, smem, st, a);
     if (e != cudaSuccess || a.splits == 1)
         return e;
     return launch_overlapped(adapter_grad_sum_kernel<XT>, dim3(a.tiles * (64 * RP / THREADS), a.G), THREADS, 0, st, a, RP);

@@ -1,4 +1,5 @@
 // extern "C" entry points: argument checks, format resolution, dispatch.
+#include <float.h>
 #include <math.h>
 #include <cmath>
 #include <string.h>
@@ -1524,7 +1525,8 @@ fpq_status fpq_adamw_step(const fpq_adamw_tensor* tensors_host, int32_t count, i
     if (!options_host || !step || (count > 0 && !tensors_host))
         return FPQ_ERR_NULL;
     const fpq_adamw_options& o = *options_host;
-    if (!std::isfinite(o.lr) || !std::isfinite(o.weight_decay) || !std::isfinite(o.eps) || o.eps < 0 || !(o.beta1 >= 0 && o.beta1 < 1) ||
+    if (!std::isfinite(o.lr) || !std::isfinite(o.weight_decay) || !std::isfinite(o.eps) || o.eps < 0 ||
+        (o.eps > 0 && o.eps < FLT_MIN) || !(o.beta1 >= 0 && o.beta1 < 1) ||
         !(o.beta2 >= 0 && o.beta2 < 1))
         return FPQ_ERR_SHAPE;
     if (!aligned(step, 8) || !aligned(factors, 4))

@@ -32,7 +32,7 @@ def call(count=1, g_type=fpq.FP32, copy_type=fpq.BF16, state_type=fpq.FP32, step
 @pytest.mark.parametrize("given,error", [
     ({"g_type": 3}, "ERR_UNSUPPORTED"), ({"copy_type": fpq.FP32}, "ERR_UNSUPPORTED"), ({"state_type": fpq.BF16}, "ERR_UNSUPPORTED"),
     ({"count": -1}, "ERR_SHAPE"), ({"lr": math.inf}, "ERR_SHAPE"), ({"beta1": 1.0}, "ERR_SHAPE"), ({"beta1": -0.1}, "ERR_SHAPE"),
-    ({"beta2": math.nan}, "ERR_SHAPE"), ({"eps": -1e-8}, "ERR_SHAPE"), ({"eps": math.nan}, "ERR_SHAPE"), ({"weight_decay": math.inf}, "ERR_SHAPE"),
+    ({"beta2": math.nan}, "ERR_SHAPE"), ({"eps": -1e-8}, "ERR_SHAPE"), ({"eps": math.nan}, "ERR_SHAPE"), ({"eps": 1e-39}, "ERR_SHAPE"), ({"weight_decay": math.inf}, "ERR_SHAPE"),
     ({"tensor": {"n": -1}}, "ERR_SHAPE"), ({"tensor": {"n": 1 << 40}}, "ERR_SHAPE"), ({"count": 2, "tensor": {"n": 1 << 39}}, "ERR_SHAPE"),
     ({"step": None}, "ERR_NULL"), ({"tensors": False}, "ERR_NULL"), ({"options": False}, "ERR_NULL"), ({"tensor": {"p": None}}, "ERR_NULL"),
     ({"tensor": {"g": None}}, "ERR_NULL"), ({"tensor": {"v": None}}, "ERR_NULL"),
