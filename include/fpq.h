@@ -435,8 +435,10 @@ fpq_status fpq_round_learn_harden(const float* alpha, int64_t N, int64_t K, uint
  *            out of range); ids [S] int32.  One adapter may serve any number of segments; segments may be empty
  *   u        NULL, or [M][R] FP32 out: what fpq_adapter_backward reads
  * Sums are FP32: FP32 operands enter the tensor cores as two TF32 terms each (errors of 2^-22 of the sum of absolute
- * terms, as FP32 multiply-adds have), 16-bit operands as they are; y is rounded once.  An infinite or NaN operand gives
- * what FP32 multiply-adds give.  Nothing depends on other rows, and equal calls give equal bits.
+ * terms, as FP32 multiply-adds have), 16-bit operands as they are (with BF16, t in two terms: 2^-18 of it is left out); y is
+ * rounded once.  An infinite or NaN operand gives
+ * what FP32 multiply-adds give.  A row's result depends on its own values and the sizes of the call alone, and equal calls give
+ * equal bits.
  *
  * fpq_adapter_backward: the gradients, from dy [M][N] (rows ld_dy apart) and what forward read and kept:
  *     t[i] = scale[g] * B[g]^T dy[i],   dx[i] = base[i] + A[g]^T t[i],
@@ -456,6 +458,13 @@ fpq_status fpq_adapter_forward(const void* x, int64_t ldx, int32_t x_type, const
                                const float* scale, int32_t G, int32_t R, const int32_t* offsets, const int32_t* ids, int32_t S,
                                const void* base, int64_t ld_base, void* y, int64_t ldy, float* u, int64_t M, int64_t N, int64_t K,
                                void* stream);
+/* Which kernel fpq_adapter_forward runs for contiguous, 16-byte aligned tensors (for logs, benchmarks and tests; nothing is
+ * launched): FPQ_ADAPTER_WARPS, by warp-level MMAs on 16 to 128 rows a block; FPQ_ADAPTER_TILES, by tcgen05 MMAs on tiles of
+ * 128 rows, for requests of many rows; negative: the error that the call would return.  The first half of the backward pass is
+ * the same kernel with N and K exchanged, if dx is wanted. */
+enum { FPQ_ADAPTER_WARPS = 0, FPQ_ADAPTER_TILES = 1 };
+int32_t fpq_adapter_route(int64_t M, int64_t N, int64_t K, int32_t G, int32_t R, int32_t S, int32_t x_type, int32_t w_type,
+                          int32_t has_base);
 size_t fpq_adapter_backward_workspace_size(int64_t M, int64_t N, int64_t K, int32_t G, int32_t R, int32_t w_type);
 fpq_status fpq_adapter_backward(const void* dy, int64_t ld_dy, const void* x, int64_t ldx, int32_t x_type, const float* u,
                                 const void* a, const void* b, int32_t w_type, const float* scale, int32_t G, int32_t R,

@@ -30,6 +30,7 @@ STATIC_SCRATCH_BYTES = 8 << 20
 SAT_PAPER, SAT_NATIVE = 0, 1
 LINEAR, CONV2D = 0, 1
 FP32, BF16, FP16, E4M3_BLOCK32 = 0, 1, 2, 3
+ADAPTER_WARPS, ADAPTER_TILES = 0, 1
 PATH_AUTO, PATH_FUSED, PATH_TWO_KERNELS, PATH_TWO_KERNELS_NARROW = 0, 1, 2, 3
 
 
@@ -81,7 +82,7 @@ EXPORTS = [
     "fpq_zero_census", "fpq_prepared_size_split", "fpq_prepare_weight_split", "fpq_conv2d_split_workspace_size",
     "fpq_conv2d_split", "fpq_set_path_policy", "fpq_get_path_policy", "fpq_read_status", "fpq_status_string",
     "fpq_conv2d_route", "fpq_linear_contraction", "fpq_conv2d_contraction", "fpq_selftest_bounded_wait",
-    "fpq_adapter_forward", "fpq_adapter_backward_workspace_size", "fpq_adapter_backward", "fpq_adamw_step",
+    "fpq_adapter_forward", "fpq_adapter_route", "fpq_adapter_backward_workspace_size", "fpq_adapter_backward", "fpq_adamw_step",
 ]
 
 _lib = None
@@ -171,6 +172,8 @@ def lib() -> ctypes.CDLL:
         L.fpq_conv2d_contraction.argtypes = [i32] * 9 + [F, F]
         L.fpq_adapter_forward.restype = i32
         L.fpq_adapter_forward.argtypes = [vp, i64, i32, vp, vp, i32, vp, i32, i32, vp, vp, i32, vp, i64, vp, i64, vp, i64, i64, i64, vp]
+        L.fpq_adapter_route.restype = i32
+        L.fpq_adapter_route.argtypes = [i64, i64, i64, i32, i32, i32, i32, i32, i32]
         L.fpq_adapter_backward_workspace_size.restype = sz
         L.fpq_adapter_backward_workspace_size.argtypes = [i64, i64, i64, i32, i32, i32]
         L.fpq_adapter_backward.restype = i32
@@ -495,6 +498,14 @@ def fpq_adapter_forward(x: torch.Tensor, a: torch.Tensor, b: torch.Tensor, offse
     if code:
         raise FpqError(code, "fpq_adapter_forward")
     return y
+
+
+def fpq_adapter_route(M: int, N: int, K: int, G: int, R: int, S: int, x_type: int, w_type: int, has_base: bool = True) -> int:
+    """Which kernel fpq_adapter_forward would run for contiguous tensors of these sizes (ADAPTER_*)."""
+    r = lib().fpq_adapter_route(M, N, K, G, R, S, x_type, w_type, int(has_base))
+    if r < 0:
+        _check(r, "fpq_adapter_route")
+    return r
 
 
 def fpq_adapter_backward_workspace_size(M: int, N: int, K: int, G: int, R: int, w_type: int) -> int:

@@ -23,99 +23,13 @@
 #include <atomic>
 #include <type_traits>
 
-#include "fpq_kernels.h"
+#include "fpq_adapter.cuh"
 
 namespace fpq {
 
 namespace {
 
 constexpr int THREADS = 256, WARPS = THREADS / 32;
-
-__device__ __forceinline__ float as_float(float v) { return v; }
-__device__ __forceinline__ float as_float(__nv_bfloat16 v) { return __bfloat162float(v); }
-__device__ __forceinline__ float as_float(__half v) { return __half2float(v); }
-template <typename T>
-__device__ __forceinline__ T from_float(float v);
-template <>
-__device__ __forceinline__ float from_float<float>(float v) { return v; }
-template <>
-__device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
-template <>
-__device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
-
-__device__ __forceinline__ void unpack(uint32_t w, float* v, __nv_bfloat16)
-{
-    v[0] = __uint_as_float(w << 16);
-    v[1] = __uint_as_float(w & 0xffff0000u);
-}
-__device__ __forceinline__ void unpack(uint32_t w, float* v, __half)
-{
-    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
-    v[0] = f.x;
-    v[1] = f.y;
-}
-
-// n values that lie side by side (n = 4 or 8), as they lie: 32-bit words of one FP32 or two 16-bit values.  They are
-// looked into only where they are used: a conversion behind each load would wait for it.
-template <typename T, int n>
-struct Raw {
-    static constexpr int WORDS = n * (int)sizeof(T) / 4;
-    uint32_t w[WORDS];
-
-    __device__ __forceinline__ void clear()
-    {
-#pragma unroll
-        for (int i = 0; i < WORDS; ++i)
-            w[i] = 0;
-    }
-    __device__ __forceinline__ void values(float (&v)[n]) const
-    {
-#pragma unroll
-        for (int i = 0; i < n; ++i)
-            if constexpr (sizeof(T) == 4) {
-                v[i] = __uint_as_float(w[i]);
-            } else if (i % 2 == 0) {
-                unpack(w[i / 2], v + i, T());
-            }
-    }
-};
-
-// Values [col, col + n) of a row of `width`; those behind its end are zeros.  VEC: the row starts at a multiple of 16 bytes
-// (of 8, for four 16-bit values) and its width is a multiple of what a vector holds.
-template <bool VEC, int n, typename T>
-__device__ __forceinline__ void load_cols(const T* row, int64_t col, int64_t width, bool there, Raw<T, n>& r)
-{
-    if constexpr (VEC) {
-        constexpr int PIECE = sizeof(T) == 4 ? 4 : n;
-#pragma unroll
-        for (int i = 0; i < n; i += PIECE) {
-            uint32_t* w = r.w + i * (int)sizeof(T) / 4;
-            if (there && col + i < width) {
-                if constexpr (PIECE * sizeof(T) == 16) {
-                    const uint4 q = *reinterpret_cast<const uint4*>(row + col + i);
-                    w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
-                } else {
-                    const uint2 q = *reinterpret_cast<const uint2*>(row + col + i);
-                    w[0] = q.x; w[1] = q.y;
-                }
-            } else {
-#pragma unroll
-                for (int k = 0; k < PIECE * (int)sizeof(T) / 4; ++k)
-                    w[k] = 0;
-            }
-        }
-    } else {
-        r.clear();
-#pragma unroll
-        for (int i = 0; i < n; ++i)
-            if (there && col + i < width) {
-                if constexpr (sizeof(T) == 4)
-                    r.w[i] = __float_as_uint(row[col + i]);
-                else
-                    r.w[i / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(row)[col + i] << (16 * (i % 2));
-            }
-    }
-}
 
 __device__ __forceinline__ uint32_t high(float x) { return (__float_as_uint(x) + 0x1000u) & 0xffffe000u; }
 __device__ __forceinline__ uint32_t low(float x, uint32_t hi) { return __float_as_uint(x - __uint_as_float(hi)); }
@@ -188,74 +102,7 @@ __device__ __forceinline__ void split_four(const float (&v)[4], uint32_t (&h)[4]
     }
 }
 
-// two values as BF16, and what is left of them
-__device__ __forceinline__ void split_bf16(float a, float b, uint32_t& h, uint32_t& l)
-{
-    const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
-    const float2 f = __bfloat1622float2(v);
-    const __nv_bfloat162 r = __floats2bfloat162_rn(a - f.x, b - f.y);
-    h = *reinterpret_cast<const uint32_t*>(&v);
-    l = *reinterpret_cast<const uint32_t*>(&r);
-}
-
-template <typename T>
-constexpr bool WIDE = sizeof(T) == 4;
-
-__device__ __forceinline__ bool finite(float v) { return (__float_as_uint(v) & 0x7f800000u) != 0x7f800000u; }
-
-// ---- which rows a tile has ---------------------------------------------------------------------------------------
-// Segment s (rows offsets[s] .. offsets[s + 1]) owns the tiles from offsets[s] / BM + s on: as many as it needs, whatever
-// its rows, and the grid of M / BM + S tiles is known without reading the offsets.  All lanes get the same answer.
-struct TileRows {
-    int64_t row;
-    int rows, id;
-};
-
-__device__ __forceinline__ TileRows find_tile(int BM, int64_t tile, const int32_t* offsets, const int32_t* ids, int S, int G, int64_t M)
-{
-    const int lane = threadIdx.x & 31;
-    TileRows r = {0, 0, -1};
-    int lo = 0, span = S;                                  // the answer is in [lo, lo + span), if there is one
-    while (true) {
-        const int step = (span + 31) / 32, s = lo + lane * step;
-        bool below = false;
-        if (s < lo + span) {
-            const int64_t o = min(max((int64_t)offsets[s], (int64_t)0), M);
-            below = (uint32_t)o / (uint32_t)BM + (int64_t)s <= tile;
-        }
-        const uint32_t votes = __ballot_sync(0xffffffffu, below);
-        if (votes == 0)
-            return r;                                      // in front of the first segment
-        const int last = 31 - __clz(votes);
-        span = min(step, lo + span - (lo + last * step));
-        lo += last * step;
-        if (step == 1)
-            break;
-    }
-    const int64_t begin = min(max((int64_t)offsets[lo], (int64_t)0), M), end = min(max((int64_t)offsets[lo + 1], (int64_t)0), M);
-    r.row = begin + (tile - ((uint32_t)begin / (uint32_t)BM + (int64_t)lo)) * BM;
-    r.rows = (int)max(min((int64_t)BM, end - r.row), (int64_t)0);
-    const int id = ids[lo];
-    r.id = id >= 0 && id < G ? id : -1;
-    return r;
-}
-
 // ---- rows to t and back ------------------------------------------------------------------------------------------
-struct RowsArgs {
-    const void* in;                // [M][D1], leading dimension ld_in
-    const void* w1;                // reduces:   [G][R][D1]
-    const void* w2;                // expands:   [G][D2][R]
-    const float* scale;            // [G] or NULL
-    const int32_t *offsets, *ids;
-    const void* base;              // [M][D2] or NULL
-    void* out;                     // [M][D2] or NULL
-    float* kept;                   // [M][R] or NULL: t (forward), s t (backward)
-    int64_t M, D1, D2, ld_in, ld_base, ld_out;
-    int G, R, S;
-    int kept_scaled;
-    int wr;                        // row groups of a block: 1, 2, 4 or 8
-};
-
 __device__ __forceinline__ void copy_async16(uint32_t dst, const void* src, bool there)
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
@@ -712,6 +559,22 @@ __device__ __forceinline__ void store_gradient(const GradArgs& a, int id, bool i
         a.da[((int64_t)id * a.R + j) * a.K + col] = v;
 }
 
+// Over how many of the a.splits blocks adapter `id`'s rows are spread: its share of all rows, so that adapters of unequal length end together
+__device__ __forceinline__ int splits_of(const GradArgs& a, int id)
+{
+    if (a.splits == 1 || a.G == 1)
+        return a.splits;
+    int64_t mine = 0, all = 0;
+    for (int sg = 0; sg < a.S; ++sg) {
+        const int other = a.ids[sg], n = min(max(a.offsets[sg + 1], 0), (int)a.M) - min(max(a.offsets[sg], 0), (int)a.M);
+        if (n > 0 && other >= 0 && other < a.G) {
+            all += n;
+            mine += other == id ? n : 0;
+        }
+    }
+    return all == 0 ? 1 : max((int)((mine * a.splits + all - 1) / all), 1);
+}
+
 template <typename XT>
 __global__ void __launch_bounds__(THREADS) adapter_grad_sum_kernel(const GradArgs a, int RP)
 {
@@ -724,11 +587,14 @@ __global__ void __launch_bounds__(THREADS) adapter_grad_sum_kernel(const GradArg
     col += (is_b ? tile - a.tiles_k : tile) * 64;
     if (col >= (is_b ? a.N : a.K) || j >= a.R)
         return;
+    const int splits = splits_of(a, id);
+    if (splits == 1)
+        return;                                            // the block itself has stored them
     const int64_t step = (int64_t)a.G * a.tiles * 64 * RP;
     const float* s = a.sums + ((int64_t)id * a.tiles + tile) * 64 * RP + i;
     float v = 0.f;
 #pragma unroll 8
-    for (int z = 0; z < a.splits; ++z)
+    for (int z = 0; z < splits; ++z)
         v += s[z * step];
     store_gradient<XT>(a, id, is_b, col, j, v);
 }
@@ -761,7 +627,9 @@ __global__ void __launch_bounds__(THREADS, 2) adapter_grad_kernel(const GradArgs
     const XT* wide = (const XT*)(is_b ? a.dy : a.x);
     const float* thin = is_b ? a.u : a.t;
     const int R = a.R, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
-    const int wn = warp % WN, wk = warp / WN, workers = WK * (int)gridDim.z, worker = (int)blockIdx.z * WK + wk, j0 = wn * JT;
+    const int wn = warp % WN, wk = warp / WN, splits = splits_of(a, id), workers = WK * splits, worker = (int)blockIdx.z * WK + wk, j0 = wn * JT;
+    if ((int)blockIdx.z >= splits)
+        return;
     uint8_t* ring = reinterpret_cast<uint8_t*>(smem4) + warp * (STAGES * Ring::STAGE);
 
     // the runs of this warp, in order: every workers-th of all runs of the adapter's segments
@@ -987,7 +855,7 @@ __global__ void __launch_bounds__(THREADS, 2) adapter_grad_kernel(const GradArgs
 #pragma unroll
         for (int k = 0; k < WK; ++k)
             v += parts[(k * 64 + col) * RP + j];
-        if (gridDim.z > 1)
+        if (splits > 1)
             sums[i] = v;
         else if (c0 + col < D && j < R)
             store_gradient<XT>(a, id, is_b, c0 + col, j, v);
@@ -1071,6 +939,9 @@ cudaError_t launch_rows_type(const RowsArgs& a, cudaStream_t st)
 
 cudaError_t launch_rows(const RowsArgs& a, int x_type, int w_type, cudaStream_t st)
 {
+    bool tiles = adapter_tiles_preferred(a, x_type, w_type);
+    if (tiles)
+        return launch_adapter_tiles(a, x_type, w_type, st) == FPQ_OK ? cudaSuccess : cudaErrorUnknown;
     if (x_type == FPQ_BF16)
         return launch_rows_type<__nv_bfloat16, __nv_bfloat16>(a, st);
     if (x_type == FPQ_FP16)
@@ -1084,10 +955,12 @@ int padded_rank(int R) { return R <= 16 ? 16 : R <= 32 ? 32 : R <= 64 ? 64 : 128
 
 int column_tiles(int64_t n) { return (int)((n + 63) / 64); }
 
-// How often the rows are split: two blocks for every SM, and 64 rows at least for a block's eight warps
+// How often the rows are split: two blocks for every SM, and 64 rows at least for a block's eight warps.  Of several adapters each gets
+// its share of that (splits_of); the sums have room for four times as many blocks.
 int grad_splits(int64_t M, int64_t N, int64_t K, int G)
 {
-    const int64_t blocks = (int64_t)(column_tiles(K) + column_tiles(N)) * G, most = std::min<int64_t>(M / 64, 2 * 148 / blocks);
+    const int64_t tiles = column_tiles(K) + column_tiles(N), rounded_up = std::min(G - 1, 8) / 2;
+    const int64_t most = std::min(M / 64, std::min(2 * 148 / tiles - rounded_up, 8 * 148 / (tiles * G)));
     return (int)std::max<int64_t>(most, 1);
 }
 
@@ -1133,6 +1006,17 @@ cudaError_t launch_adapter_forward(const AdapterProblem& p, const void* x, int64
     a.M = p.M; a.D1 = p.K; a.D2 = p.N; a.ld_in = ldx; a.ld_base = ld_base; a.ld_out = ldy;
     a.G = p.G; a.R = p.R; a.S = p.S;
     return launch_rows(a, p.x_type, p.w_type, st);
+}
+
+bool adapter_forward_by_tiles(const AdapterProblem& p, bool base)
+{
+    const void* there = reinterpret_cast<const void*>((uintptr_t)256);      // never followed: only alignment is looked at
+    RowsArgs a = {};
+    a.in = a.w1 = a.w2 = there;
+    a.out = (void*)there;
+    a.base = base ? there : nullptr;
+    a.M = p.M; a.D1 = a.ld_in = p.K; a.D2 = a.ld_out = a.ld_base = p.N; a.G = p.G; a.R = p.R; a.S = p.S;
+    return p.M > 0 && p.S > 0 && adapter_tiles_preferred(a, p.x_type, p.w_type);
 }
 
 // workspace: t [M][R] FP32, A and B transposed, the sums of the blocks that share an adapter's rows

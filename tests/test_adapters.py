@@ -99,9 +99,10 @@ def segments(t):
 
 
 def product_error(D, terms):
-    """Error of a sum of D products relative to the sum of their magnitudes: two TF32 terms each (2^-22 left out, 2^-23 of each second term
-    cut off), at most `terms` cut-off additions of the tensor cores, each 2^-23 at most, and the FP32 additions behind them."""
-    return 2.0 ** -21 + (terms + 20 + D / 64) * 2.0 ** -23
+    """Error of a sum of D products relative to the sum of their magnitudes: two TF32 terms each (where the first term is the number cut off,
+    the second is below 2^-10 of it: their product, 2^-20, is left out, and of each second term 2^-10 of it is cut off, 2^-20 twice), at
+    most `terms` cut-off additions of the tensor cores, each 2^-23 at most, and the FP32 additions behind them."""
+    return 3 * 2.0 ** -20 + (terms + 20 + D / 64) * 2.0 ** -23
 
 
 def half_step(t, v):
@@ -181,6 +182,74 @@ TYPES = [(F32, F32), (F32, BF), (F32, HF), (BF, BF), (HF, HF)]
 def test_forward(shape, xt, wt):
     t = make(*shape, xt=xt, wt=wt)
     check_forward(t, *run_forward(t))
+
+
+# requests of many rows: tiles of 128 rows on tcgen05 MMAs, in clusters of two blocks or alone, forward or (N and K exchanged) backward
+TALL = [
+    (8192, 640, 1280, 64, [0, 8192], [0], 1),
+    (8000, 648, 1288, 56, [7, 3000, 3000, 7990], [1, 0, 0], 2),
+    (9000, 1288, 640, 32, [0, 1, 4400, 8999], [1, 0, 1], 2),
+    (9400, 648, 1288, 24, [0, 4600, 9400], [0, -1], 1),
+    (18900, 1288, 648, 16, [3, 18899], [1], 2),
+    (18931, 640, 1280, 32, [0, 18931], [0], 1),
+    (12000, 64, 1032, 40, [5, 6000, 11990], [0, 1], 2),
+]
+
+
+def by_tiles(shape, xt, wt):
+    M, K, N, R, cuts, _, G = shape
+    kind = {F32: fpq.FP32, BF: fpq.BF16, HF: fpq.FP16}
+    return [fpq.fpq_adapter_route(M, n, k, G, R, len(cuts) - 1, kind[xt], kind[wt], base) == fpq.ADAPTER_TILES
+            for n, k, base in ((N, K, True), (N, K, False), (K, N, True))]
+
+
+TALL_CASES = [(s, x, w) for s in TALL for x, w in TYPES if any(by_tiles(s, x, w))]
+
+
+def test_tall_requests_reach_their_kernel():
+    """Every type and padded rank that the kernel is built for is among the cases, forward and backward."""
+    seen = {(x, w, max(16, 1 << (s[3] - 1).bit_length()), way) for s, x, w in TALL_CASES for way, yes in enumerate(by_tiles(s, x, w)) if yes}
+    for x, w in TYPES:
+        for rp in (32, 64) if x == F32 else (16, 32, 64):
+            assert {way for a, b, r, way in seen if (a, b, r) == (x, w, rp)} >= {0, 2}, (x, w, rp)
+    assert not any(by_tiles((8192, 640, 640, 128, [0, 8192], [0], 1), F32, F32))
+    with pytest.raises(fpq.FpqError, match="shape"):
+        fpq.fpq_adapter_route(1, 1, 1, 1, 200, 1, fpq.FP32, fpq.FP32)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape,xt,wt", TALL_CASES, ids=lambda s: "x".join(map(str, s[:4])) if isinstance(s, tuple) else str(s)[6:])
+def test_tall_requests(shape, xt, wt):
+    t = make(*shape, xt=xt, wt=wt)
+    check_forward(t, *run_forward(t))
+    check_forward(t, *run_forward(t, base=False), base=False)
+    M, K, R = t["x"].shape[0], t["x"].shape[1], t["a"].shape[1]
+    u = torch.randn(M, R, device="cuda")
+    dx = t["dbase"].clone()
+    before = dx.clone()
+    _, da, db = fpq.fpq_adapter_backward(t["dy"], t["x"], u, t["a"], t["b"], t["offsets"], t["ids"], t["scale"], dx, dx)
+    check_backward(t, u, dx, da, db, before)
+    assert fpq.fpq_read_status() == fpq.OK
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("xt", [F32, BF])
+def test_tall_requests_in_slices_and_with_odd_values(xt):
+    shape = (9300, 320, 1032, 64, [0, 9290], [0], 1)
+    assert all(by_tiles(shape, xt, xt)[:2])
+    t = make(*shape, xt, xt, ldx=704, ldy=1160)
+    check_forward(t, *run_forward(t, ldy=1160))
+    clean = run_forward(t)[1].clone()
+    t["x"][3, 17], t["x"][200, 0], t["x"][9289, 5] = float("inf"), float("nan"), 3e38
+    t["x"][9290:] = float("nan")
+    before, y, u = run_forward(t)
+    keep = torch.ones(9300, dtype=torch.bool, device="cuda")
+    keep[[3, 200, 9289]] = False
+    assert torch.equal(y[keep], clean[keep]) and bool(torch.isnan(y[200]).all())
+    for r in (3, 9289):
+        want = t["x"][r].float().cpu() @ t["a"][0].float().cpu().T
+        assert torch.equal(torch.isnan(u[r].cpu()), torch.isnan(want)) and torch.equal(torch.isinf(u[r].cpu()), torch.isinf(want))
+    assert fpq.fpq_read_status() == fpq.OK
 
 
 @pytest.mark.gpu
