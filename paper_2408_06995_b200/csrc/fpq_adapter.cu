@@ -112,14 +112,64 @@ __device__ __forceinline__ void copy_async4(uint32_t dst, const void* src, bool 
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(there ? 4 : 0) : "memory");
 }
 
+// The 16-byte pieces at src of N rows (`every` rows and src_step, dst_step apart; of the first `rows` of them) to shared memory, `there`
+// values of each and zeros behind: words asynchronously where the rows allow it, otherwise through registers, all loads in front
+// of the stores.  Out of line: the path for rows at multiples of 16 bytes stays in the instruction cache.
+template <typename XT, int N>
+__device__ __noinline__ void copy_pieces(uint8_t* dst, int dst_step, const XT* src, int64_t src_step, int rows, int every, int there, int by,
+                                         const void* anywhere)
+{
+    constexpr int PER = 16 / (int)sizeof(XT);
+    if (by >= 4 && (sizeof(XT) == 4 || there >= PER || (there & 1) == 0)) {
+#pragma unroll
+        for (int k = 0; k < N; ++k)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const bool some = k * every < rows && i * (4 / (int)sizeof(XT)) < there;
+                copy_async4(smem_u32(dst + k * dst_step + 4 * i), some ? src + k * src_step + i * (4 / (int)sizeof(XT)) : (const XT*)anywhere, some);
+            }
+        return;
+    }
+    uint32_t w[N][4];
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
+        const uint16_t* p = reinterpret_cast<const uint16_t*>(src + k * src_step);
+        const bool some = k * every < rows;
+        if (some && there >= PER && (reinterpret_cast<uintptr_t>(p) & 3) == 0) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                w[k][i] = reinterpret_cast<const uint32_t*>(p)[i];
+        } else if (some && there >= PER) {
+            // between words: the first value, three words, the last value
+            const uint32_t a = p[0], b = *reinterpret_cast<const uint32_t*>(p + 1), c = *reinterpret_cast<const uint32_t*>(p + 3),
+                           d = *reinterpret_cast<const uint32_t*>(p + 5), e = p[7];
+            w[k][0] = a | b << 16;
+            w[k][1] = __funnelshift_l(b, c, 16);
+            w[k][2] = __funnelshift_l(c, d, 16);
+            w[k][3] = d >> 16 | e << 16;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                w[k][i] = (some && 2 * i < there ? (uint32_t)p[2 * i] : 0u) | (some && 2 * i + 1 < there ? (uint32_t)p[2 * i + 1] << 16 : 0u);
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+        *reinterpret_cast<uint4*>(dst + k * dst_step) = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
+}
+
 // A warp's share of 32 columns of a row: for FP32 rows, columns 4 q .. and 16 + 4 q .. (q = lane % 4), for 16-bit rows 8 q ..: a vector per
 // lane, the vectors of a row side by side.
 template <typename XT>
 __device__ __forceinline__ int group_column(int q, int i) { return sizeof(XT) == 4 ? (i >> 2) * 16 + 4 * q + (i & 3) : 8 * q + i; }
 
 template <typename XT, bool VEC, typename T>
-__device__ __forceinline__ void load_group(const T* row, int c0, int q, int width, bool there, Raw<T, 8>& r)
+__device__ __forceinline__ void load_group(const T* row, int c0, int q, int width, bool there, Raw<T, 8>& r, bool vec = true)
 {
+    if (!VEC && vec) {
+        load_group<XT, true>(row, c0, q, width, there, r);
+        return;
+    }
     if constexpr (sizeof(XT) == 4) {
         Raw<T, 4> a, b;
         load_cols<VEC>(row, c0 + 4 * q, width, there, a);
@@ -169,8 +219,9 @@ __global__ void __launch_bounds__(THREADS, RP <= 64 ? 2 : 1) adapter_rows_kernel
     const int r0 = (warp & (WR - 1)) * 16, wk = warp / WR, here = tr.rows - r0;
     const float s = a.scale && tr.id >= 0 ? a.scale[tr.id] : 1.f;
     const int D1 = (int)a.D1, D2 = (int)a.D2, R = a.R, step = 32 * WK * (int)C, first = 32 * ((int)rank * WK + wk);
-    const WT* w1 = (const WT*)a.w1 + (int64_t)max(tr.id, 0) * R * D1;
-    const WT* w2 = (const WT*)a.w2 + (int64_t)max(tr.id, 0) * R * D2;
+    const int ld1 = (int)a.ld_w1, ld2 = (int)a.ld_w2;
+    const WT* w1 = (const WT*)a.w1 + (int64_t)max(tr.id, 0) * R * ld1;
+    const WT* w2 = (const WT*)a.w2 + (int64_t)max(tr.id, 0) * D2 * ld2;
     const XT* in = (const XT*)a.in + tr.row * a.ld_in;
 
     // what comes through the ring: groups of x, then groups of base
@@ -188,19 +239,24 @@ __global__ void __launch_bounds__(THREADS, RP <= 64 ? 2 : 1) adapter_rows_kernel
             const int i = is_x ? fetched : fetched - xs, col = first + i * step + cc * PER, width = is_x ? D1 : D2;
             const int64_t ld = is_x ? a.ld_in : a.ld_base;
             const XT* src = (is_x ? x_from : b_from) + (int64_t)i * step;
-            uint8_t* slot = ring + put * Ring::SLOT;
+            // FP32: eight vectors a row; the halves of odd rows are exchanged, so that two rows' vectors lie in different banks
+            uint8_t* dst = ring + put * Ring::SLOT + cr * (32 * (int)sizeof(XT)) + (sizeof(XT) == 4 ? cc ^ ((cr & 1) << 2) : cc) * 16;
+            if constexpr (VEC) {
 #pragma unroll
-            for (int k = 0; k < 16; k += EVERY) {
-                // FP32: eight vectors a row; the halves of odd rows are exchanged, so that two rows' vectors lie in different banks
-                const int r = cr + k, c = sizeof(XT) == 4 ? cc ^ ((r & 1) << 2) : cc;
-                uint8_t* dst = slot + r * (32 * (int)sizeof(XT)) + c * 16;
-                if constexpr (VEC) {
-                    const bool there = r < here && col < width;
-                    copy_async16(smem_u32(dst), there ? src + k * ld : in, there);
+                for (int k = 0; k < 16; k += EVERY) {
+                    const bool there = cr + k < here && col < width;
+                    copy_async16(smem_u32(dst + k * (32 * (int)sizeof(XT))), there ? src + k * ld : in, there);
+                }
+            } else {
+                const int by = is_x ? a.in_by : a.base_by;
+                if (by == 16) {
+#pragma unroll 1
+                    for (int k = 0; k < 16; k += EVERY) {
+                        const bool there = cr + k < here && col < width;
+                        copy_async16(smem_u32(dst + k * (32 * (int)sizeof(XT))), there ? src + k * ld : in, there);
+                    }
                 } else {
-#pragma unroll
-                    for (int e = 0; e < PER; ++e)
-                        reinterpret_cast<XT*>(dst)[e] = r < here && col + e < width ? src[k * ld + e] : from_float<XT>(0.f);
+                    copy_pieces<XT, 16 / EVERY>(dst, EVERY * 32 * (int)sizeof(XT), src, EVERY * ld, here - cr, EVERY, width - col, by, in);
                 }
             }
         }
@@ -231,51 +287,57 @@ __global__ void __launch_bounds__(THREADS, RP <= 64 ? 2 : 1) adapter_rows_kernel
     if (tr.id >= 0) {
         float acc[NT][4] = {}, part[NT][4] = {};
         Raw<XT, 8> x[2];
-        Raw<WT, 8> w[NT], w_next[AHEAD ? NT : 1];
-        const WT* w_row = w1 + (int64_t)g * D1;
+        constexpr int BATCH = NT > 4 && !NATIVE ? 4 : NT;      // (more at a time do not fit the registers)
+        Raw<WT, 8> w_next[AHEAD ? NT : 1];
+        const WT* w_row = w1 + (int64_t)g * ld1;
         int since = 0;
         if (AHEAD && xs > 0)
 #pragma unroll
             for (int n = 0; n < NT; ++n)
-                load_group<XT, VEC>(w_row + (int64_t)(n * 8) * D1, first, q, D1, n * 8 + g < R, w_next[n]);
+                load_group<XT, VEC>(w_row + (int64_t)(n * 8) * ld1, first, q, D1, n * 8 + g < R, w_next[n], a.vec_w1);
         for (int i = 0; i < xs; ++i) {
             const int k0 = first + i * step;
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
-                if (AHEAD) {
-                    w[n] = w_next[n];
-                    load_group<XT, VEC>(w_row + (int64_t)(n * 8) * D1, k0 + step, q, D1, n * 8 + g < R, w_next[n]);   // (behind the end nothing is loaded)
-                } else {
-                    load_group<XT, VEC>(w_row + (int64_t)(n * 8) * D1, k0, q, D1, n * 8 + g < R, w[n]);
-                }
-            take(x);
-            if constexpr (NATIVE) {
+            for (int n0 = 0; n0 < NT; n0 += BATCH) {
+                Raw<WT, 8> w[BATCH];
 #pragma unroll
-                for (int st = 0; st < 2; ++st) {
-                    const uint32_t v[4] = {x[0].w[2 * st], x[1].w[2 * st], x[0].w[2 * st + 1], x[1].w[2 * st + 1]};
-#pragma unroll
-                    for (int n = 0; n < NT; ++n)
-                        mma_16(part[n], v, w[n].w[2 * st], w[n].w[2 * st + 1], XT());
-                }
-            } else {
-                float f[2][8], fw[NT][8];
-                x[0].values(f[0]);
-                x[1].values(f[1]);
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-                    w[n].values(fw[n]);
-#pragma unroll
-                for (int st = 0; st < 4; ++st) {
-                    const float v[4] = {f[0][2 * st], f[1][2 * st], f[0][2 * st + 1], f[1][2 * st + 1]};
-                    uint32_t vh[4], vl[4];
-                    split_four<true>(v, vh, vl);
-                    float b[NT][2];
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        b[n][0] = fw[n][2 * st];
-                        b[n][1] = fw[n][2 * st + 1];
+                for (int n = 0; n < BATCH; ++n)
+                    if (AHEAD) {
+                        w[n] = w_next[n];
+                        load_group<XT, VEC>(w_row + (int64_t)(n * 8) * ld1, k0 + step, q, D1, n * 8 + g < R, w_next[n], a.vec_w1);   // (behind the end nothing is loaded)
+                    } else {
+                        load_group<XT, VEC>(w_row + (int64_t)((n0 + n) * 8) * ld1, k0, q, D1, (n0 + n) * 8 + g < R, w[n], a.vec_w1);
                     }
-                    mma_split<true, WIDE<WT>, NT>(part, vh, vl, b);
+                if (n0 == 0)
+                    take(x);
+                if constexpr (NATIVE) {
+#pragma unroll
+                    for (int st = 0; st < 2; ++st) {
+                        const uint32_t v[4] = {x[0].w[2 * st], x[1].w[2 * st], x[0].w[2 * st + 1], x[1].w[2 * st + 1]};
+#pragma unroll
+                        for (int n = 0; n < BATCH; ++n)
+                            mma_16(part[n0 + n], v, w[n].w[2 * st], w[n].w[2 * st + 1], XT());
+                    }
+                } else {
+                    float f[2][8], fw[BATCH][8];
+                    x[0].values(f[0]);
+                    x[1].values(f[1]);
+#pragma unroll
+                    for (int n = 0; n < BATCH; ++n)
+                        w[n].values(fw[n]);
+#pragma unroll
+                    for (int st = 0; st < 4; ++st) {
+                        const float v[4] = {f[0][2 * st], f[1][2 * st], f[0][2 * st + 1], f[1][2 * st + 1]};
+                        uint32_t vh[4], vl[4];
+                        split_four<true>(v, vh, vl);
+                        float b[BATCH][2];
+#pragma unroll
+                        for (int n = 0; n < BATCH; ++n) {
+                            b[n][0] = fw[n][2 * st];
+                            b[n][1] = fw[n][2 * st + 1];
+                        }
+                        mma_split<true, WIDE<WT>, BATCH>(part + n0, vh, vl, b);
+                    }
                 }
             }
             if (++since == 2) {                            // 64 columns
@@ -321,7 +383,7 @@ __global__ void __launch_bounds__(THREADS, RP <= 64 ? 2 : 1) adapter_rows_kernel
             if (!finite(v) && r < tr.rows && j < R) {
                 v = 0.f;
                 for (int k = 0; k < D1; ++k)
-                    v = fmaf(as_float(in[r * a.ld_in + k]), as_float(w1[(int64_t)j * D1 + k]), v);
+                    v = fmaf(as_float(in[r * a.ld_in + k]), as_float(w1[(int64_t)j * ld1 + k]), v);
             }
             if (a.kept && rank == 0 && r < tr.rows && j < R)
                 a.kept[(tr.row + r) * R + j] = a.kept_scaled ? v * s : v;
@@ -378,7 +440,10 @@ __global__ void __launch_bounds__(THREADS, RP <= 64 ? 2 : 1) adapter_rows_kernel
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int n = c0 + n0 + tile_column(e);
-                load_cols<VEC>(w2 + (int64_t)n * R, (b * 4 + q) * TPER, R, n < D2, w[e]);
+                if (VEC || a.vec_w2)
+                    load_cols<true>(w2 + (int64_t)n * ld2, (b * 4 + q) * TPER, R, n < D2, w[e]);
+                else
+                    load_cols<false>(w2 + (int64_t)n * ld2, (b * 4 + q) * TPER, R, n < D2, w[e]);
             }
         };
         Raw<WT, TPER> w_next[AHEAD2 ? BLOCKS : 1][4];
@@ -440,7 +505,7 @@ __global__ void __launch_bounds__(THREADS, RP <= 64 ? 2 : 1) adapter_rows_kernel
                         if (!finite(v) && r < tr.rows && col < D2) {
                             v = 0.f;
                             for (int j = 0; j < R; ++j)
-                                v = fmaf(t_smem[r * PITCH + j], as_float(w2[(int64_t)col * R + j]), v);
+                                v = fmaf(t_smem[r * PITCH + j], as_float(w2[(int64_t)col * ld2 + j]), v);
                         }
                     }
                 }
@@ -466,7 +531,7 @@ __global__ void __launch_bounds__(THREADS, RP <= 64 ? 2 : 1) adapter_rows_kernel
 #pragma unroll
                 for (int p = 0; p < 8; p += PER) {
                     const int col = group_column<XT>(q, p);
-                    if (VEC) {
+                    if (VEC || a.out_by == 16) {
                         if (c0 + col < D2) {
                             alignas(16) XT v[PER];
 #pragma unroll
@@ -489,28 +554,29 @@ __global__ void __launch_bounds__(THREADS, RP <= 64 ? 2 : 1) adapter_rows_kernel
         cluster_wait();                                    // nobody still reads this block's sums
 }
 
-// Adapters transposed for the backward pass: src [G][rows][cols] to dst [G][cols][rows], 32 x 32 at a time.
+// Adapters transposed for the backward pass, 32 x 32 at a time: [G][R][K] to [G][K][ldr] and [G][N][R] to [G][R][ldn], rows of which start
+// at multiples of 16 bytes, zeros behind their ends.
 template <typename T>
-__global__ void __launch_bounds__(THREADS) transpose_adapters_kernel(const T* a, T* at, const T* b, T* bt, int R, int K, int N, int tiles_a, int tiles)
+__global__ void __launch_bounds__(THREADS) transpose_adapters_kernel(const T* a, T* at, const T* b, T* bt, int R, int K, int N, int ldr, int ldn,
+                                                                     int tiles_a, int tiles)
 {
     __shared__ T piece[32][33];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int g = blockIdx.x / tiles, t = blockIdx.x % tiles;
     const bool is_b = t >= tiles_a;
-    const int rows = is_b ? N : R, cols = is_b ? R : K, across = (cols + 31) / 32, i = is_b ? t - tiles_a : t;
+    const int rows = is_b ? N : R, cols = is_b ? R : K, ld = is_b ? ldn : ldr, across = (cols + 31) / 32, i = is_b ? t - tiles_a : t;
     const T* src = (is_b ? b : a) + (int64_t)g * rows * cols;
-    T* dst = (is_b ? bt : at) + (int64_t)g * rows * cols;
+    T* dst = (is_b ? bt : at) + (int64_t)g * cols * ld;
     const int x = threadIdx.x & 31, y = threadIdx.x >> 5, r0 = i / across * 32, c0 = i % across * 32;
 #pragma unroll
     for (int k = y; k < 32; k += 8)
-        if (r0 + k < rows && c0 + x < cols)
-            piece[k][x] = src[(int64_t)(r0 + k) * cols + c0 + x];
+        piece[k][x] = r0 + k < rows && c0 + x < cols ? src[(int64_t)(r0 + k) * cols + c0 + x] : T(0);
     __syncthreads();
 #pragma unroll
     for (int k = y; k < 32; k += 8)
-        if (c0 + k < cols && r0 + x < rows)
-            dst[(int64_t)(c0 + k) * rows + r0 + x] = piece[x][k];
+        if (c0 + k < cols && r0 + x < ld)
+            dst[(int64_t)(c0 + k) * ld + r0 + x] = piece[x][k];
 }
 
 // ---- gradients of the adapters -----------------------------------------------------------------------------------
@@ -524,7 +590,7 @@ struct GradArgs {
     const int32_t *offsets, *ids;
     float *da, *db;                // [G][R][K], [G][N][R]
     int64_t M, N, K, ldx, ld_dy;
-    int G, R, S;
+    int G, R, S, x_by, dy_by;
     int tiles_k, tiles;            // column tiles of dA; those behind them are dB's
     float* sums;                   // [split][G][tiles][64 RP] where the rows are split
     int splits;
@@ -559,18 +625,24 @@ __device__ __forceinline__ void store_gradient(const GradArgs& a, int id, bool i
         a.da[((int64_t)id * a.R + j) * a.K + col] = v;
 }
 
-// Over how many of the a.splits blocks adapter `id`'s rows are spread: its share of all rows, so that adapters of unequal length end together
+// Over how many of the a.splits blocks adapter `id`'s rows are spread: its share of all rows, so that adapters of unequal length end together.
+// Called by whole warps.
 __device__ __forceinline__ int splits_of(const GradArgs& a, int id)
 {
     if (a.splits == 1 || a.G == 1)
         return a.splits;
     int64_t mine = 0, all = 0;
-    for (int sg = 0; sg < a.S; ++sg) {
+    for (int sg = threadIdx.x & 31; sg < a.S; sg += 32) {
         const int other = a.ids[sg], n = min(max(a.offsets[sg + 1], 0), (int)a.M) - min(max(a.offsets[sg], 0), (int)a.M);
         if (n > 0 && other >= 0 && other < a.G) {
             all += n;
             mine += other == id ? n : 0;
         }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        all += __shfl_xor_sync(0xffffffffu, all, o);
+        mine += __shfl_xor_sync(0xffffffffu, mine, o);
     }
     return all == 0 ? 1 : max((int)((mine * a.splits + all - 1) / all), 1);
 }
@@ -585,11 +657,9 @@ __global__ void __launch_bounds__(THREADS) adapter_grad_sum_kernel(const GradArg
     int col, j;
     tile_element(i, RP, is_b, col, j);
     col += (is_b ? tile - a.tiles_k : tile) * 64;
-    if (col >= (is_b ? a.N : a.K) || j >= a.R)
-        return;
     const int splits = splits_of(a, id);
-    if (splits == 1)
-        return;                                            // the block itself has stored them
+    if (splits == 1 || col >= (is_b ? a.N : a.K) || j >= a.R)
+        return;                                            // (with one, the block itself has stored them)
     const int64_t step = (int64_t)a.G * a.tiles * 64 * RP;
     const float* s = a.sums + ((int64_t)id * a.tiles + tile) * 64 * RP + i;
     float v = 0.f;
@@ -610,15 +680,17 @@ struct GradRing {
     static constexpr int STAGES = sizeof(XT) == 2 && JT == 32 ? 3 : 2;                            // two blocks on an SM
 };
 
-// JT: ranks of a warp; RP / JT warps share a run of rows.  VEC: rows of x and dy by 16 bytes; the thin rows by 16 bytes if R % 4 == 0.
-template <typename XT, int RP, int JT, bool VEC>
+// JT: ranks of a warp; RP / JT warps share a run of rows.
+template <typename XT, int RP, int JT>
 __global__ void __launch_bounds__(THREADS, 2) adapter_grad_kernel(const GradArgs a)
 {
     using Ring = GradRing<XT, JT>;
     constexpr int NT = JT / 8, WN = RP / JT, WK = WARPS / WN, RUN = Ring::RUN, STAGES = Ring::STAGES;
     constexpr int MB = 4 / NT < 1 ? 1 : 4 / NT;            // four independent MMAs one after the other
+    constexpr int CHAIN = NT >= 4 ? 1 : 2;
     extern __shared__ float4 smem4[];
-    float* parts = reinterpret_cast<float*>(smem4);        // at the end: [WK][64][RP]
+    constexpr int PITCH = RP + 2;                          // (columns of a tile in different banks, for the writes and for the reads)
+    float* parts = reinterpret_cast<float*>(smem4);        // at the end: [WK][64][PITCH]
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int tile = blockIdx.x, id = blockIdx.y;
@@ -633,19 +705,32 @@ __global__ void __launch_bounds__(THREADS, 2) adapter_grad_kernel(const GradArgs
     uint8_t* ring = reinterpret_cast<uint8_t*>(smem4) + warp * (STAGES * Ring::STAGE);
 
     // the runs of this warp, in order: every workers-th of all runs of the adapter's segments
-    int sg = -1, runs = 0;                                 // runs of the segments in front, modulo the workers
+    int chunk = -32, my_begin = 0, my_end = 0;             // 32 segments at a time, one to a lane
+    uint32_t left = 0;
+    int runs = 0;                                          // runs of the segments in front, modulo the workers
     int at = 0, n_runs = 0, begin = 0, end = 0;
     auto next_run = [&](int& row, int& rows) {
         while (at >= n_runs) {
             runs = (runs + n_runs) % workers;
             n_runs = 0;
-            do
-                if (++sg >= a.S)
+            while (left == 0) {
+                chunk += 32;
+                if (chunk >= a.S)
                     return false;
-            while (a.ids[sg] != id);
-            begin = min(max(a.offsets[sg], 0), (int)a.M);
-            end = min(max(a.offsets[sg + 1], 0), (int)a.M);
-            n_runs = end > begin ? (end - begin - 1) / RUN + 1 : 0;
+                const int sg = chunk + lane;
+                bool mine = false;
+                if (sg < a.S) {
+                    my_begin = min(max(a.offsets[sg], 0), (int)a.M);
+                    my_end = min(max(a.offsets[sg + 1], 0), (int)a.M);
+                    mine = a.ids[sg] == id && my_end > my_begin;
+                }
+                left = __ballot_sync(0xffffffffu, mine);
+            }
+            const int from = __ffs(left) - 1;
+            left &= left - 1;
+            begin = __shfl_sync(0xffffffffu, my_begin, from);
+            end = __shfl_sync(0xffffffffu, my_end, from);
+            n_runs = (end - begin - 1) / RUN + 1;
             at = worker - runs + (worker < runs ? workers : 0);
         }
         row = begin + at * RUN;
@@ -656,6 +741,7 @@ __global__ void __launch_bounds__(THREADS, 2) adapter_grad_kernel(const GradArgs
     constexpr int PER = 16 / (int)sizeof(XT), ACROSS = 64 / PER, EVERY = 32 / ACROSS;      // vectors of a row, rows at a time
     const int wr = lane / ACROSS, wc = lane % ACROSS * PER;
     const bool wide_in = c0 + wc < D;
+    const int by = is_b ? a.dy_by : a.x_by;
     constexpr int T_ACROSS = JT / 4, T_EVERY = 32 / T_ACROSS;
     const int tr = lane / T_ACROSS, tc = lane % T_ACROSS * 4;
     const bool thin_in = j0 + tc < R;
@@ -666,16 +752,17 @@ __global__ void __launch_bounds__(THREADS, 2) adapter_grad_kernel(const GradArgs
             uint8_t* w = ring + slot * Ring::STAGE;
             const XT* src = wide + (int64_t)(row + wr) * ld + c0 + wc;
             uint8_t* dst = w + wr * Ring::WIDE_PITCH + wc * (int)sizeof(XT);
+            if (by == 16) {
 #pragma unroll
-            for (int k = 0; k < RUN; k += EVERY) {
-                if constexpr (VEC) {
+                for (int k = 0; k < RUN; k += EVERY) {
                     const bool there = wide_in && wr + k < rows;
                     copy_async16(smem_u32(dst + k * Ring::WIDE_PITCH), there ? src + k * ld : wide, there);
-                } else {
-#pragma unroll
-                    for (int e = 0; e < PER; ++e)
-                        reinterpret_cast<XT*>(dst + k * Ring::WIDE_PITCH)[e] = wr + k < rows && c0 + wc + e < D ? src[k * ld + e] : from_float<XT>(0.f);
                 }
+            } else {
+#pragma unroll 1
+                for (int k = 0; k < RUN; k += 4 * EVERY)
+                    copy_pieces<XT, 4>(dst + k * Ring::WIDE_PITCH, EVERY * Ring::WIDE_PITCH, src + k * ld, EVERY * ld, rows - wr - k, EVERY,
+                                       (int)min(D - c0 - wc, (int64_t)PER), by, wide);
             }
             uint8_t* t = w + RUN * Ring::WIDE_PITCH;
             if (R % 4 == 0) {
@@ -771,11 +858,11 @@ __global__ void __launch_bounds__(THREADS, 2) adapter_grad_kernel(const GradArgs
             }
         } else {
 #pragma unroll
-            for (int s0 = 0; s0 < RUN / 8; s0 += 2) {      // 16 rows: a sum starts from zero, and is added in registers
-                uint32_t ph[2][NT][2], pl[2][NT][2];
-                float v[2][2][8];                          // [rows 2 q, 2 q + 1][both columns of the MMA's four row tiles]
+            for (int s0 = 0; s0 < RUN / 8; s0 += CHAIN) {  // a sum of 8 or 16 rows starts from zero, and is added in registers
+                uint32_t ph[CHAIN][NT][2], pl[CHAIN][NT][2];
+                float v[CHAIN][2][8];                          // [rows 2 q, 2 q + 1][both columns of the MMA's four row tiles]
 #pragma unroll
-                for (int st = 0; st < 2; ++st)
+                for (int st = 0; st < CHAIN; ++st)
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         const int row = 8 * (s0 + st) + 2 * q + h;
@@ -801,7 +888,7 @@ __global__ void __launch_bounds__(THREADS, 2) adapter_grad_kernel(const GradArgs
                 for (int m0 = 0; m0 < 4; m0 += MB) {
                     float part[MB][NT][4];
 #pragma unroll
-                    for (int st = 0; st < 2; ++st) {
+                    for (int st = 0; st < CHAIN; ++st) {
                         uint32_t wh[MB][4], wl[MB][4];
 #pragma unroll
                         for (int i = 0; i < MB; ++i) {
@@ -844,7 +931,7 @@ __global__ void __launch_bounds__(THREADS, 2) adapter_grad_kernel(const GradArgs
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int col = sizeof(XT) == 4 ? h * 32 + g * 4 + m : g * 8 + 2 * m + h;
-                *reinterpret_cast<float2*>(parts + (wk * 64 + col) * RP + j0 + n * 8 + 2 * q) = make_float2(acc[m][n][2 * h], acc[m][n][2 * h + 1]);
+                *reinterpret_cast<float2*>(parts + (wk * 64 + col) * PITCH + j0 + n * 8 + 2 * q) = make_float2(acc[m][n][2 * h], acc[m][n][2 * h + 1]);
             }
     __syncthreads();
     float* sums = a.sums + (((int64_t)blockIdx.z * a.G + id) * a.tiles + tile) * 64 * RP;
@@ -854,7 +941,7 @@ __global__ void __launch_bounds__(THREADS, 2) adapter_grad_kernel(const GradArgs
         float v = 0.f;
 #pragma unroll
         for (int k = 0; k < WK; ++k)
-            v += parts[(k * 64 + col) * RP + j];
+            v += parts[(k * 64 + col) * PITCH + j];
         if (splits > 1)
             sums[i] = v;
         else if (c0 + col < D && j < R)
@@ -904,6 +991,12 @@ bool vectors(const void* p, int64_t ld, int64_t width, int bytes)
 
 int type_bytes(int t) { return t == FPQ_FP32 ? 4 : 2; }
 
+// bytes at a time that rows allow: 16, 4 (words), or 2 where rows of 16-bit values start between words
+int bytes_at_a_time(const void* p, int64_t ld, int64_t width, int bytes)
+{
+    return vectors(p, ld, width, bytes) ? 16 : (uintptr_t)p % 4 == 0 && ld * bytes % 4 == 0 ? 4 : 2;
+}
+
 template <typename XT, typename WT, int RP, bool VEC>
 cudaError_t launch_rows_as(RowsArgs a, cudaStream_t st)
 {
@@ -925,13 +1018,18 @@ cudaError_t launch_rows_as(RowsArgs a, cudaStream_t st)
     return launch_cluster<RowsArgs>(adapter_rows_kernel<XT, WT, RP, VEC>, known, MOST, dim3((unsigned)(tiles * c)), c, smem, st, a);
 }
 
+// VEC: everything is read and written by vectors; otherwise each operand as its rows allow.  (Weight rows longer than needed hold zeros
+// behind their ends.)
 template <typename XT, typename WT>
-cudaError_t launch_rows_type(const RowsArgs& a, cudaStream_t st)
+cudaError_t launch_rows_type(RowsArgs a, cudaStream_t st)
 {
-    const int xb = sizeof(XT), wb = sizeof(WT), ranks = a.R <= 16 ? 4 : 8;
-    const bool vec = vectors(a.in, a.ld_in, a.D1, xb) && vectors(a.w1, a.D1, a.D1, wb) &&
-                     (!a.out || (vectors(a.out, a.ld_out, a.D2, xb) && (!a.base || vectors(a.base, a.ld_base, a.D2, xb)) &&
-                                 a.R % ranks == 0 && (uintptr_t)a.w2 % 16 == 0));
+    constexpr int XB = sizeof(XT);
+    a.in_by = bytes_at_a_time(a.in, a.ld_in, a.D1, XB);
+    a.base_by = a.base ? bytes_at_a_time(a.base, a.ld_base, a.D2, XB) : 16;
+    a.out_by = a.out ? bytes_at_a_time(a.out, a.ld_out, a.D2, XB) : 16;
+    a.vec_w2 = (uintptr_t)a.w2 % 16 == 0 && a.ld_w2 % (a.R <= 16 ? 4 : 8) == 0 && (a.R % (a.R <= 16 ? 4 : 8) == 0 || a.ld_w2 > a.R);
+    a.vec_w1 = vectors(a.w1, a.ld_w1, a.ld_w1, sizeof(WT));
+    const bool vec = a.vec_w1 && (!a.out || a.vec_w2) && a.in_by == 16 && a.base_by == 16 && a.out_by == 16;
 #define FPQ_ROWS(RP) (vec ? launch_rows_as<XT, WT, RP, true>(a, st) : launch_rows_as<XT, WT, RP, false>(a, st))
     return a.R <= 16 ? FPQ_ROWS(16) : a.R <= 32 ? FPQ_ROWS(32) : a.R <= 64 ? FPQ_ROWS(64) : FPQ_ROWS(128);
 #undef FPQ_ROWS
@@ -964,13 +1062,13 @@ int grad_splits(int64_t M, int64_t N, int64_t K, int G)
     return (int)std::max<int64_t>(most, 1);
 }
 
-template <typename XT, int RP, int JT, bool VEC>
+template <typename XT, int RP, int JT>
 cudaError_t launch_grad_as(const GradArgs& a, cudaStream_t st)
 {
     using Ring = GradRing<XT, JT>;
-    const size_t smem = std::max<size_t>((size_t)(WARPS / (RP / JT)) * 64 * RP * 4, (size_t)WARPS * Ring::STAGES * Ring::STAGE);
+    const size_t smem = std::max<size_t>((size_t)(WARPS / (RP / JT)) * 64 * (RP + 2) * 4, (size_t)WARPS * Ring::STAGES * Ring::STAGE);
     static std::atomic<uint64_t> known{0};
-    const cudaError_t e = launch_cluster<GradArgs>(adapter_grad_kernel<XT, RP, JT, VEC>, known, (int)smem, dim3(a.tiles, a.G, a.splits), 1, smem, st, a);
+    const cudaError_t e = launch_cluster<GradArgs>(adapter_grad_kernel<XT, RP, JT>, known, (int)smem, dim3(a.tiles, a.G, a.splits), 1, smem, st, a);
     if (e != cudaSuccess || a.splits == 1)
         return e;
     return launch_overlapped(adapter_grad_sum_kernel<XT>, dim3(a.tiles * (64 * RP / THREADS), a.G), THREADS, 0, st, a, RP);
@@ -979,18 +1077,22 @@ cudaError_t launch_grad_as(const GradArgs& a, cudaStream_t st)
 template <typename XT>
 cudaError_t launch_grad(const GradArgs& a, cudaStream_t st)
 {
-    const bool vec = vectors(a.x, a.ldx, a.K, sizeof(XT)) && vectors(a.dy, a.ld_dy, a.N, sizeof(XT));
-#define FPQ_GRAD(RP, JT) (vec ? launch_grad_as<XT, RP, JT, true>(a, st) : launch_grad_as<XT, RP, JT, false>(a, st))
-    return a.R <= 16 ? FPQ_GRAD(16, 16) : a.R <= 32 ? FPQ_GRAD(32, 32) : a.R <= 64 ? FPQ_GRAD(64, 32) : FPQ_GRAD(128, 32);
-#undef FPQ_GRAD
+    return a.R <= 16   ? launch_grad_as<XT, 16, 16>(a, st)
+           : a.R <= 32 ? launch_grad_as<XT, 32, 32>(a, st)
+           : a.R <= 64 ? launch_grad_as<XT, 64, 32>(a, st)
+                       : launch_grad_as<XT, 128, 32>(a, st);
 }
+
+// rows of the transposed adapters, in elements: [G][K][ldr] and [G][R][ldn]
+int padded_ranks(int R, int bytes) { return (int)round_up(R, bytes == 4 && R <= 16 ? 4 : 8); }
+int padded_columns(int64_t N, int bytes) { return (int)round_up(N, 16 / bytes); }
 
 template <typename T>
 cudaError_t launch_transpose_as(const AdapterProblem& p, T* at, T* bt, cudaStream_t st)
 {
     const int64_t r = (p.R + 31) / 32, tiles_a = r * ((p.K + 31) / 32), tiles = tiles_a + r * ((p.N + 31) / 32);
     return launch_overlapped(transpose_adapters_kernel<T>, dim3((unsigned)(tiles * p.G)), THREADS, 0, st, (const T*)p.a, at, (const T*)p.b, bt,
-                             p.R, (int)p.K, (int)p.N, (int)tiles_a, (int)tiles);
+                             p.R, (int)p.K, (int)p.N, padded_ranks(p.R, sizeof(T)), padded_columns(p.N, sizeof(T)), (int)tiles_a, (int)tiles);
 }
 
 size_t pad16(size_t n) { return (n + 15) / 16 * 16; }
@@ -1003,6 +1105,7 @@ cudaError_t launch_adapter_forward(const AdapterProblem& p, const void* x, int64
     RowsArgs a = {};
     a.in = x; a.w1 = p.a; a.w2 = p.b; a.scale = p.scale; a.offsets = p.offsets; a.ids = p.ids;
     a.base = base; a.out = y; a.kept = u;
+    a.ld_w1 = p.K; a.ld_w2 = p.R;
     a.M = p.M; a.D1 = p.K; a.D2 = p.N; a.ld_in = ldx; a.ld_base = ld_base; a.ld_out = ldy;
     a.G = p.G; a.R = p.R; a.S = p.S;
     return launch_rows(a, p.x_type, p.w_type, st);
@@ -1015,6 +1118,7 @@ bool adapter_forward_by_tiles(const AdapterProblem& p, bool base)
     a.in = a.w1 = a.w2 = there;
     a.out = (void*)there;
     a.base = base ? there : nullptr;
+    a.ld_w1 = p.K; a.ld_w2 = p.R;
     a.M = p.M; a.D1 = a.ld_in = p.K; a.D2 = a.ld_out = a.ld_base = p.N; a.G = p.G; a.R = p.R; a.S = p.S;
     return p.M > 0 && p.S > 0 && adapter_tiles_preferred(a, p.x_type, p.w_type);
 }
@@ -1022,10 +1126,10 @@ bool adapter_forward_by_tiles(const AdapterProblem& p, bool base)
 // workspace: t [M][R] FP32, A and B transposed, the sums of the blocks that share an adapter's rows
 size_t adapter_backward_bytes(int64_t M, int64_t N, int64_t K, int G, int R, int w_type)
 {
-    const size_t wb = type_bytes(w_type), g = (size_t)G * R * wb;
+    const size_t wb = type_bytes(w_type), g = (size_t)G * wb;
     const int splits = grad_splits(M, N, K, G);
     const size_t sums = splits == 1 ? 0 : (size_t)splits * G * (column_tiles(K) + column_tiles(N)) * 64 * padded_rank(R) * 4;
-    return pad16((size_t)M * R * 4) + pad16(g * K) + pad16(g * N) + sums;
+    return pad16((size_t)M * R * 4) + pad16(g * K * padded_ranks(R, (int)wb)) + pad16(g * R * padded_columns(N, (int)wb)) + sums;
 }
 
 cudaError_t launch_adapter_backward(const AdapterProblem& p, const void* dy, int64_t ld_dy, const void* x, int64_t ldx, const float* u,
@@ -1034,9 +1138,10 @@ cudaError_t launch_adapter_backward(const AdapterProblem& p, const void* dy, int
 {
     float* t = (float*)workspace;
     const size_t wb = type_bytes(p.w_type);
+    const int xb = type_bytes(p.x_type);
     uint8_t* at = (uint8_t*)workspace + pad16((size_t)p.M * p.R * 4);
-    uint8_t* bt = at + pad16((size_t)p.G * p.R * p.K * wb);
-    float* sums = (float*)(bt + pad16((size_t)p.G * p.R * p.N * wb));
+    uint8_t* bt = at + pad16((size_t)p.G * p.K * padded_ranks(p.R, (int)wb) * wb);
+    float* sums = (float*)(bt + pad16((size_t)p.G * p.R * padded_columns(p.N, (int)wb) * wb));
     if (p.M > 0 && p.S > 0) {
         cudaError_t e = wb == 4 ? launch_transpose_as(p, (uint32_t*)at, (uint32_t*)bt, st)
                                                   : launch_transpose_as(p, (uint16_t*)at, (uint16_t*)bt, st);
@@ -1045,6 +1150,7 @@ cudaError_t launch_adapter_backward(const AdapterProblem& p, const void* dy, int
         RowsArgs a = {};
         a.in = dy; a.w1 = bt; a.w2 = at; a.scale = p.scale; a.offsets = p.offsets; a.ids = p.ids;
         a.base = base; a.out = dx; a.kept = t; a.kept_scaled = 1;
+        a.ld_w1 = padded_columns(p.N, (int)wb); a.ld_w2 = padded_ranks(p.R, (int)wb);
         a.M = p.M; a.D1 = p.N; a.D2 = p.K; a.ld_in = ld_dy; a.ld_base = ld_base; a.ld_out = ld_dx;
         a.G = p.G; a.R = p.R; a.S = p.S;
         e = launch_rows(a, p.x_type, p.w_type, st);
@@ -1054,6 +1160,8 @@ cudaError_t launch_adapter_backward(const AdapterProblem& p, const void* dy, int
     GradArgs b = {};
     b.x = x; b.dy = dy; b.t = t; b.u = u; b.scale = p.scale; b.offsets = p.offsets; b.ids = p.ids; b.da = da; b.db = db;
     b.M = p.M; b.N = p.N; b.K = p.K; b.ldx = ldx; b.ld_dy = ld_dy; b.G = p.G; b.R = p.R; b.S = p.M > 0 ? p.S : 0;
+    b.x_by = bytes_at_a_time(x, ldx, p.K, xb);
+    b.dy_by = bytes_at_a_time(dy, ld_dy, p.N, xb);
     b.tiles_k = column_tiles(p.K);
     b.tiles = b.tiles_k + column_tiles(p.N);
     b.sums = sums;

@@ -84,14 +84,24 @@ __device__ __forceinline__ void load_cols(const T* row, int64_t col, int64_t wid
         }
     } else {
         r.clear();
+        const T* p = row + col;
+        if (sizeof(T) == 2 && (reinterpret_cast<uintptr_t>(p) & 3) == 0) {
 #pragma unroll
-        for (int i = 0; i < n; ++i)
-            if (there && col + i < width) {
-                if constexpr (sizeof(T) == 4)
-                    r.w[i] = __float_as_uint(row[col + i]);
-                else
-                    r.w[i / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(row)[col + i] << (16 * (i % 2));
-            }
+            for (int i = 0; i < n; i += 2)
+                if (there && col + i + 1 < width)
+                    r.w[i / 2] = *reinterpret_cast<const uint32_t*>(p + i);
+                else if (there && col + i < width)
+                    r.w[i / 2] = reinterpret_cast<const uint16_t*>(p)[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < n; ++i)
+                if (there && col + i < width) {
+                    if constexpr (sizeof(T) == 4)
+                        r.w[i] = __float_as_uint(p[i]);
+                    else
+                        r.w[i / 2] |= (uint32_t)reinterpret_cast<const uint16_t*>(p)[i] << (16 * (i % 2));
+                }
+        }
     }
 }
 
@@ -160,6 +170,9 @@ struct RowsArgs {
     int G, R, S;
     int kept_scaled;
     int wr;                        // row groups of a block: 1, 2, 4 or 8
+    int64_t ld_w1, ld_w2;          // rows of the weights: adapter g's start g R ld_w1 and g D2 ld_w2 elements behind the first
+    int in_by, base_by, out_by;    // bytes at a time that the rows allow: 16, 4 or 2
+    int vec_w1, vec_w2;            // the weights' rows allow vectors
 };
 
 // The pass on tcgen05 MMAs for requests of many rows (fpq_adapter_tile.cu): whether it applies and is expected to be faster than

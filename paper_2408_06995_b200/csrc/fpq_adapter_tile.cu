@@ -331,8 +331,8 @@ __global__ void __launch_bounds__(TileLayout<XT, WT, RP>::THREADS, 1) adapter_ti
         // ---------------- sixteen warps ----------------
         const int w = warp - 2, tid = threadIdx.x - 64, quarter = warp & 3, group = w >> 2, row = quarter * 32 + lane;
         const int rows_here = tr.rows - quarter * 32;      // of this warp's 32
-        const WT* w1 = (const WT*)a.w1 + (int64_t)max(tr.id, 0) * R * D1;
-        const WT* w2 = (const WT*)a.w2 + (int64_t)max(tr.id, 0) * R * D2;
+        const WT* w1 = (const WT*)a.w1 + (int64_t)max(tr.id, 0) * R * a.ld_w1;
+        const WT* w2 = (const WT*)a.w2 + (int64_t)max(tr.id, 0) * D2 * a.ld_w2;
         uint8_t* slots = smem + T::SLOT_BASE + w * SLOTS * SLOT_BYTES;
         const uint32_t slots_addr = base_addr + T::SLOT_BASE + w * SLOTS * SLOT_BYTES, my_full = slot_full + 8 * SLOTS * w;
 
@@ -438,7 +438,7 @@ __global__ void __launch_bounds__(TileLayout<XT, WT, RP>::THREADS, 1) adapter_ti
                         v = 0.f;
 #pragma unroll 1
                         for (int k = 0; k < D1; ++k)
-                            v = fmaf(as_float(x[k]), as_float(w1[(int64_t)j * D1 + k]), v);
+                            v = fmaf(as_float(x[k]), as_float(w1[j * a.ld_w1 + k]), v);
                         mine[j - group * SHARE] = v;
                     }
                 }
@@ -566,7 +566,7 @@ __global__ void __launch_bounds__(TileLayout<XT, WT, RP>::THREADS, 1) adapter_ti
                         float v = 0.f;
 #pragma unroll 1
                         for (int k = 0; k < R; ++k)
-                            v = fmaf(t[k], as_float(w2[(int64_t)(col + i) * R + k]), v);
+                            v = fmaf(t[k], as_float(w2[(col + i) * a.ld_w2 + k]), v);
                         reinterpret_cast<XT*>(sl + swizzled(lane, i / PER))[i % PER] = from_float<XT>((b ? as_float(b[i]) : 0.f) + v);
                     }
                 }
@@ -662,11 +662,11 @@ fpq_status launch_as(const RowsArgs& a, int x_type, int w_type, cudaStream_t st)
     const bool raw1 = T::FP32 && !T::WIDE_W, raw2 = !T::BF && !T::WIDE_W;
     if (!encode(enc, &tx, a.in, a.M, a.D1, a.ld_in, x_type, TILE_M, xe, true) || !encode(enc, &ty, out, a.M, width, ld, x_type, 32, xe, true) ||
         !encode(enc, &tb, a.out && a.base ? a.base : out, a.M, width, a.out && a.base ? a.ld_base : ld, x_type, 32, xe, true) ||
-        !encode(enc, &t1, a.w1, (int64_t)a.G * a.R, a.D1, a.D1, w_type, RP, raw1 ? 32 : xe, !raw1))
+        !encode(enc, &t1, a.w1, (int64_t)a.G * a.R, a.D1, a.ld_w1, w_type, RP, raw1 ? 32 : xe, !raw1))
         return FPQ_ERR_CUDA;
     if (!a.out)
         t2 = t1;
-    else if (!encode(enc, &t2, a.w2, (int64_t)a.G * a.D2, a.R, a.R, w_type, NCOLS, raw2 ? RP : 128 / (int)sizeof(WT), !raw2))
+    else if (!encode(enc, &t2, a.w2, (int64_t)a.G * a.D2, a.R, a.ld_w2, w_type, NCOLS, raw2 ? RP : 128 / (int)sizeof(WT), !raw2))
         return FPQ_ERR_CUDA;
     // FP32 accumulators; operands BF16 (1), FP16 (0) or TF32 (2), K-major; M = 128, N = the rank, or 64 columns
     const uint32_t f1 = x_type == FPQ_FP32 ? 2 : x_type == FPQ_BF16 ? 1 : 0, f2 = T::BF ? 1 : 2;
@@ -715,7 +715,7 @@ bool adapter_tiles_preferred(const RowsArgs& a, int x_type, int w_type)
         (a.out && a.base && !mapped(a.base, a.ld_base, bytes)))
         return false;
     const int wb = w_type == FPQ_FP32 ? 4 : 2;
-    if (!mapped(a.w1, a.D1, wb) || (a.out && !mapped(a.w2, a.R, wb)) || (int64_t)a.G * std::max<int64_t>(a.R, a.out ? a.D2 : 0) >= ((int64_t)1 << 31))
+    if (!mapped(a.w1, a.ld_w1, wb) || (a.out && !mapped(a.w2, a.ld_w2, wb)) || (int64_t)a.G * std::max<int64_t>(a.R, a.out ? a.D2 : 0) >= ((int64_t)1 << 31))
         return false;
     // Estimates of both passes in us, fitted to 234 shapes of 1024 to 65536 rows (26 % and 20 % rms; the choice costs 3 % over the better
     // one, the pass by warps alone 21 %).  This one: a wave of blocks has its own latency and 36 bytes per ns and block; the pass by
