@@ -450,7 +450,7 @@ fpq_status fpq_round_learn_harden(const float* alpha, int64_t N, int64_t K, uint
  *   workspace  fpq_adapter_backward_workspace_size bytes (0 for sizes out of range), 16-byte aligned, contents not kept
  * One kernel forward, three backward, on `stream`; no allocation, no synchronisation.  Pointers are aligned to their
  * element; rows at multiples of 16 bytes are read 16 bytes at a time.  Limits: M and S below 2^31 and 2^24, N and K
- * up to 2^24, G up to 65535, G * R * max(N, K) below 2^40.  M = 0 or S = 0: forward does nothing, backward writes zeros to
+ * up to 2^24, G up to 65535, G * R * max(N, K) below 2^40, G * (N + K) below 2^33.  M = 0 or S = 0: forward does nothing, backward writes zeros to
  * da and db.  Errors: FPQ_ERR_UNSUPPORTED, FPQ_ERR_SHAPE, FPQ_ERR_NULL, FPQ_ERR_ALIGN, FPQ_ERR_WORKSPACE, FPQ_ERR_CUDA.
  */
 enum { FPQ_FP32 = 0, FPQ_BF16 = 1, FPQ_FP16 = 2, FPQ_E4M3_BLOCK32 = 3 };

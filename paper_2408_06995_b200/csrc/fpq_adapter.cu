@@ -744,7 +744,7 @@ __global__ void __launch_bounds__(THREADS, 2) adapter_grad_kernel(const GradArgs
     const int by = is_b ? a.dy_by : a.x_by;
     constexpr int T_ACROSS = JT / 4, T_EVERY = 32 / T_ACROSS;
     const int tr = lane / T_ACROSS, tc = lane % T_ACROSS * 4;
-    const bool thin_in = j0 + tc < R;
+    const bool thin_in = j0 + tc < R, thin_vec = R % 4 == 0 && (reinterpret_cast<uintptr_t>(thin) & 15) == 0;
     auto fetch = [&](int slot) {
         int row, rows;
         const bool some = next_run(row, rows);
@@ -765,7 +765,7 @@ __global__ void __launch_bounds__(THREADS, 2) adapter_grad_kernel(const GradArgs
                                        (int)min(D - c0 - wc, (int64_t)PER), by, wide);
             }
             uint8_t* t = w + RUN * Ring::WIDE_PITCH;
-            if (R % 4 == 0) {
+            if (thin_vec) {
                 const float* from = thin + (int64_t)(row + tr) * R + j0 + tc;
 #pragma unroll
                 for (int k = 0; k < RUN; k += T_EVERY) {

@@ -166,7 +166,6 @@ __global__ void __launch_bounds__(TileLayout<XT, WT, RP>::THREADS, 1) adapter_ti
                    w_full = bars + 136, w_empty = bars + 168, w_ready = bars + 200, y_full = bars + 232, slot_full = bars + 264;   // slot_full: [warp][SLOTS]
     volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(smem + T::BARS + 480);
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     uint32_t rank = cluster_rank(), C;
@@ -213,6 +212,8 @@ __global__ void __launch_bounds__(TileLayout<XT, WT, RP>::THREADS, 1) adapter_ti
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
+    // (behind the allocation: a block of the next kernel that moves in could otherwise hold the tensor memory that this one waits for)
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const uint32_t tmem = *tmem_slot;
     bool dead = false;
 

@@ -1433,7 +1433,8 @@ static fpq_status check_adapters(const AdapterProblem& p)
         return FPQ_ERR_UNSUPPORTED;
     const int64_t most = (int64_t)1 << 24;
     if (p.M < 0 || p.M > 0x7fffffff || p.S < 0 || p.S > most || p.N < 1 || p.N > most || p.K < 1 || p.K > most || p.G < 1 ||
-        p.G > 65535 || p.R < 1 || p.R > 128 || (int64_t)p.G * p.R * (p.N > p.K ? p.N : p.K) >= ((int64_t)1 << 40))
+        p.G > 65535 || p.R < 1 || p.R > 128 || (int64_t)p.G * p.R * (p.N > p.K ? p.N : p.K) >= ((int64_t)1 << 40) ||
+        (int64_t)p.G * (p.N + p.K) >= ((int64_t)1 << 33))
         return FPQ_ERR_SHAPE;
     return FPQ_OK;
 }

@@ -351,6 +351,25 @@ def test_tiny_and_huge_moments():
 
 
 @pytest.mark.gpu
+def test_a_tensor_of_more_than_2_to_31_elements():
+    n, tail, o = (1 << 31) + 4131, 1000, {**O, "lr": 0.5}
+    p, g = torch.zeros(n, device="cuda"), torch.zeros(n, dtype=BF, device="cuda")
+    m, v = torch.zeros(n, dtype=torch.uint8, device="cuda"), torch.zeros(n, dtype=torch.uint8, device="cuda")
+    scales = [torch.zeros(-(-n // 32), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    first = n - tail - (n - tail) % 32                    # a block's first element
+    g[first:] = torch.randn(n - first, device="cuda").bfloat16()
+    step = counter(0)
+    fpq.fpq_adamw_step(fpq.fpq_adamw_table([p], [g], [m], [v], [scales[0]], [scales[1]]), step, seed=1, **o)
+    gg = g[first:].float().cpu().numpy()
+    new_m, new_v = moments(gg, np.zeros_like(gg), np.zeros_like(gg), o)
+    check_p(p[first:].cpu().numpy(), np.zeros_like(gg), new_m, new_v, 1, o)
+    for k, s, value, which, least in ((m, scales[0], new_m, 0, 0), (v, scales[1], np.sqrt(new_v), 1, 1)):
+        c, e = encode(pad(value), noise(first, -(-len(gg) // 32) * 32, 1, 1)[which], least)
+        assert np.array_equal(k[first:].cpu().numpy(), c[:len(gg)]) and np.array_equal(s[first // 32:].cpu().numpy(), e)
+    assert not bool(p[:first].any())
+
+
+@pytest.mark.gpu
 def test_no_tensors_still_count():
     step = counter(7)
     fpq.fpq_adamw_step(fpq.fpq_adamw_table([], [], [], []), step, lr=1e-3)

@@ -36,7 +36,7 @@ BAD = [({"x_type": 3}, "ERR_UNSUPPORTED"), ({"x_type": -1}, "ERR_UNSUPPORTED"), 
        ({"x_type": fpq.BF16}, "ERR_UNSUPPORTED"), ({"x_type": fpq.FP16, "w_type": fpq.BF16}, "ERR_UNSUPPORTED"),
        ({"M": -1}, "ERR_SHAPE"), ({"M": 1 << 31}, "ERR_SHAPE"), ({"N": 0}, "ERR_SHAPE"), ({"K": 0}, "ERR_SHAPE"), ({"K": (1 << 24) + 1}, "ERR_SHAPE"),
        ({"G": 0}, "ERR_SHAPE"), ({"G": 65536}, "ERR_SHAPE"), ({"R": 0}, "ERR_SHAPE"), ({"R": 129}, "ERR_SHAPE"), ({"S": -1}, "ERR_SHAPE"),
-       ({"S": (1 << 24) + 1}, "ERR_SHAPE"), ({"ldx": 15}, "ERR_SHAPE"), ({"G": 65535, "R": 128, "N": 1 << 18}, "ERR_SHAPE"),
+       ({"S": (1 << 24) + 1}, "ERR_SHAPE"), ({"ldx": 15}, "ERR_SHAPE"), ({"G": 65535, "R": 128, "N": 1 << 18}, "ERR_SHAPE"), ({"G": 32768, "R": 1, "N": 1 << 18}, "ERR_SHAPE"),
        ({"a": None}, "ERR_NULL"), ({"b": None}, "ERR_NULL"), ({"offsets": None}, "ERR_NULL"), ({"ids": None}, "ERR_NULL"), ({"x": None}, "ERR_NULL"),
        ({"x": 4098}, "ERR_ALIGN"), ({"a": 4098}, "ERR_ALIGN"), ({"b": 4097}, "ERR_ALIGN"), ({"scale": 4098}, "ERR_ALIGN"),
        ({"offsets": 4098}, "ERR_ALIGN"), ({"ids": 4097}, "ERR_ALIGN"), ({"base": 4098}, "ERR_ALIGN"), ({"u": 4098}, "ERR_ALIGN")]
@@ -304,6 +304,52 @@ def test_forward_values_without_a_split(value):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("S,G,M", [(40, 40, 700), (1500, 300, 2600), (2500, 7, 900)])
+def test_many_segments(S, G, M):
+    """More segments than a warp looks through at a time, empty ones among them, and many adapters."""
+    g = torch.Generator().manual_seed(S)
+    cuts = [0] + torch.randint(0, M + 1, (S - 1,), generator=g).sort().values.tolist() + [M - 3]
+    cuts = [min(c, M - 3) for c in cuts]
+    ids = torch.randint(-1, G, (S,), generator=g).tolist()
+    t = make(M, 64, 72, 4, cuts, ids, G)
+    check_forward(t, *run_forward(t))
+    u = torch.randn(M, 4, device="cuda")
+    dx = torch.full((M, 64), -7.0, device="cuda")
+    before = dx.clone()
+    _, da, db = fpq.fpq_adapter_backward(t["dy"], t["x"], u, t["a"], t["b"], t["offsets"], t["ids"], t["scale"], t["dbase"], dx)
+    check_backward(t, u, dx, da, db, before)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("R", [4, 64])
+def test_offsets_beyond_32_bits(R):
+    """An output of more than 2^32 bytes and 2^31 elements: the last rows, by both kernels."""
+    M, K, N = 140000, 64, 16384
+    x = torch.randn(M, K, device="cuda").bfloat16()
+    a, b = (torch.randn(1, R, K, device="cuda") / 8).bfloat16(), (torch.randn(1, N, R, device="cuda") / 8).bfloat16()
+    offsets, ids = torch.tensor([5, M - 1], dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    y = torch.zeros(M, N, dtype=BF, device="cuda")
+    fpq.fpq_adapter_forward(x, a, b, offsets, ids, None, None, y)
+    for lo, hi in ((5, 40), (131060, 131090), (M - 40, M - 1)):
+        _, _, want, dy = rows_exact(x[lo:hi].double(), a[0].double(), b[0].double(), None, 1.0, R, BF)
+        check_rows(y[lo:hi], want, dy, "y")
+    assert not bool(y[:5].any()) and not bool(y[M - 1].any())
+    dy, u = y[:, :], torch.randn(M, R, device="cuda")
+    _, da, db = fpq.fpq_adapter_backward(dy, x, u, a, b, offsets, ids, need_dx=False)
+    ea, ta = torch.zeros(R, K, dtype=torch.float64, device="cuda"), torch.zeros(R, K, dtype=torch.float64, device="cuda")
+    for lo in range(5, M - 1, 10000):
+        rows = slice(lo, min(lo + 10000, M - 1))
+        te, dt, _, _ = rows_exact(dy[rows].double(), b[0].double().T, a[0].double().T, None, 1.0, R, BF)
+        ea += te.T @ x[rows].double()
+        ta += dt.T @ x[rows].double().abs() + product_error(M, 24) * (te.abs().T @ x[rows].double().abs())
+    check_rows(da[0], ea, ta, "da")
+    cols = torch.tensor([0, 1, 8191, N - 1], device="cuda")
+    d = dy[5:M - 1, cols].double()
+    uu = u[5:M - 1].double()
+    check_rows(db[0, cols], d.T @ uu, (product_error(M, 24) + 2.0 ** -23) * (d.abs().T @ uu.abs()), "db")
+
+
+@pytest.mark.gpu
 def test_wrong_lists_stay_in_bounds():
     """Offsets out of range are clamped and ids out of range mean no adapter: every row keeps base or gets some adapter's result."""
     t = make(50, 64, 32, 8, [-100, 20, 1000], [0, 5], 2)
@@ -402,6 +448,26 @@ def test_backward_strides_in_place_and_without_dx(xt):
     check_backward(t, u, dx, da2, db2, before)
     assert torch.equal(da, da2) and torch.equal(db, db2)
     assert not bool(da2[2].any()) and not bool(db2[2].any())          # an adapter without rows
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("xt", [F32, BF])
+def test_tensors_at_any_element(xt):
+    """Every tensor one element behind an aligned address."""
+    def behind(v):
+        flat = torch.empty(v.numel() + 1, dtype=v.dtype, device="cuda")[1:]
+        return flat.view(v.shape).copy_(v)
+
+    M, K, N, R, G = 150, 96, 64, 16, 2
+    t = {k: behind(v) for k, v in make(M, K, N, R, [0, 60, 148], [1, 0], G, xt, xt).items()}
+    y, u = behind(torch.full((M, N), -7.0, device="cuda").to(xt)), behind(torch.full((M, R), -7.0, device="cuda"))
+    before = y.clone()
+    fpq.fpq_adapter_forward(t["x"], t["a"], t["b"], t["offsets"], t["ids"], t["scale"], t["base"], y, u)
+    check_forward(t, before, y, u)
+    dx, da, db = behind(torch.full((M, K), -7.0, device="cuda").to(xt)), behind(torch.empty_like(t["a"], dtype=F32)), behind(torch.empty_like(t["b"], dtype=F32))
+    before = dx.clone()
+    fpq.fpq_adapter_backward(t["dy"], t["x"], u, t["a"], t["b"], t["offsets"], t["ids"], t["scale"], t["dbase"], dx, da, db)
+    check_backward(t, u, dx, da, db, before)
 
 
 @pytest.mark.gpu
