@@ -4,15 +4,23 @@
 //   backward  t_i = s B^T dy_i, dx_i = base_i + A^T t_i,   dA = sum_i t_i x_i^T,   dB = s sum_i dy_i u_i^T   (u_i = A x_i)
 //
 // A, B and s are those of the adapter that row i's request uses.  With a rank of 16 a row costs 2 R (K + N) operations on
-// (K + 2 N) values: bound by memory, so every kernel reads its rows once.  Forward and the first half of backward are one
-// kernel with the roles of the matrices exchanged: a block (or a cluster of up to 8, sharing the reduction and the output
-// columns) takes a tile of rows of one request, reduces it to t in shared memory and multiplies it out again.
+// (K + 2 N) values: bound by memory, so every kernel reads its rows once.
 //
-// Products run on the tensor cores as TF32 with FP32 operands split in two: x = hi + lo with 11 significant bits each, the
-// products hi hi, hi lo and lo hi (16-bit operands are TF32 numbers themselves, one term).  What is left out is 2^-22 of a
-// product.  The tensor cores cut their sums off instead of rounding them: at most 64 columns are summed there, the rest in
-// registers by FP32 additions.  Operands go from global memory straight into the registers of the MMA: the order of the
-// reduction is free, so a thread's share of a row is 8 values that lie side by side.
+// Forward and the first half of backward are one kernel with the roles of the matrices exchanged: adapter_rows_kernel, for requests of
+// many rows and ranks above 16 the tcgen05 pass of fpq_adapter_tile.cu.  A block (or a cluster of up to 8, sharing the reduction and
+// the output columns: single tokens) takes 16 to 128 rows of one request, reduces them to t in shared memory and multiplies t out
+// again.  8192 x 1280 -> 320, FP32, rank 16: 20 us, 3.2 TB/s; 64 single tokens with an adapter each, 1280 -> 1280: 7.5 us.  It spends some
+// 300 instructions on 16 x 32 values (half of the issue slots with 16 warps on an SM): operand splits, the addresses of the weights'
+// fragments, the sums.  That and the latency of a tile bound it, not the memory.
+//
+// Backward then forms dA and dB (adapter_grad_kernel): columns of x with t and of dy with u, rows split over blocks and added up in a
+// fixed order.  30011 x 1280 -> 640, BF16, rank 32, three adapters: some 45 of 99 us.  Four launches that overlap (weights transposed, rows,
+// gradients, their sums): of a small call's 13 us most is their latency.
+//
+// Products run on the tensor cores as TF32 with FP32 operands in two terms x = hi + lo of 11 significant bits each: hi hi, hi lo and
+// lo hi (16-bit operands are TF32 numbers themselves, one term, or are multiplied as they are).  Some 2^-22 of a product is left
+// out.  The tensor cores cut their sums off instead of rounding them: at most 64 columns, or 16 rows, are summed there, the rest in
+// registers by FP32 additions.  The order of a reduction is free: a thread's share of a row lies side by side.
 //
 // An infinity, or a number that rounds up to one, has no split: a result that is not finite is worked out again by FP32
 // multiply-adds.
@@ -31,6 +39,8 @@ namespace {
 
 constexpr int THREADS = 256, WARPS = THREADS / 32;
 
+// The two terms of an FP32 number: rounded to 11 significant bits, and what that leaves off (the tensor core reads 11 bits of it).  (The
+// number itself as the first term, which the tensor core cuts off, saves an instruction and no time.)
 __device__ __forceinline__ uint32_t high(float x) { return (__float_as_uint(x) + 0x1000u) & 0xffffe000u; }
 __device__ __forceinline__ uint32_t low(float x, uint32_t hi) { return __float_as_uint(x - __uint_as_float(hi)); }
 
@@ -669,8 +679,8 @@ __global__ void __launch_bounds__(THREADS) adapter_grad_sum_kernel(const GradArg
     store_gradient<XT>(a, id, is_b, col, j, v);
 }
 
-// Every warp has a ring of its own in shared memory: runs of 16 (32) rows of 64 columns and of its JT ranks, fetched
-// asynchronously STAGES - 1 runs ahead; no warp waits for another before the end.  The pitches keep a quarter warp's
+// Every warp has a ring of its own in shared memory: runs of 16 (32) rows of 64 columns and of its JT ranks, fetched asynchronously
+// STAGES - 1 runs ahead; no warp waits for another before the end.  (Loads into registers, 8192 x 1280 columns: 40 us; so, 14.)  The pitches keep a quarter warp's
 // vectors, and a warp's single words, in different banks.
 template <typename XT, int JT>
 struct GradRing {
