@@ -11,7 +11,9 @@
 //      them (the rows of a request's last tile, which are fewer, are stored by the warp).
 // Bound by memory: 18944 x 64 -> 2560, BF16, rank 64, one block for every SM: 44 us, 4.4 TB/s; the pass by warps (fpq_adapter.cu), which
 // spends some 300 instructions on 16 x 32 values, 95 us.  A wave of blocks has some 7 us of its own (finding the tile, the first copies,
-// the step from t to y): 32768 x 320 -> 2560, two waves, 83 us against 166.
+// the step from t to y).  32768 x 320 -> 2560, two blocks on an SM: 78 us against 159.
+#include <math.h>
+
 #include <algorithm>
 #include <atomic>
 #include <mutex>
@@ -27,17 +29,18 @@ namespace {
 constexpr int TILE_M = 128, NCOLS = 64;
 constexpr int X_BYTES = TILE_M * 128, SLOT_BYTES = 32 * 128;
 
-template <typename XT, typename WT, int RP>
+// TWO: two blocks on an SM, of eight working warps each; otherwise one of sixteen (of eight, where t takes 64 KB)
+template <typename XT, typename WT, int RP, bool TWO>
 struct TileLayout {
     static constexpr bool FP32 = sizeof(XT) == 4;
     static constexpr bool WIDE_W = sizeof(WT) == 4;
     static constexpr bool BF = std::is_same<XT, __nv_bfloat16>::value;              // t in two BF16 terms, otherwise TF32 terms
-    static constexpr int GROUPS = RP == 64 && !BF ? 2 : 4, WORK_WARPS = 4 * GROUPS, THREADS = 32 * (2 + WORK_WARPS);
+    static constexpr int GROUPS = TWO || (RP == 64 && !BF) ? 2 : 4, WORK_WARPS = 4 * GROUPS, THREADS = 32 * (2 + WORK_WARPS);
     static constexpr int KE = 128 / (int)sizeof(XT);                                // columns of a stage
     // W1's part of a stage: the operand as it lies in memory; FP32 rows: with its tails, or 16-bit weights and what they are in FP32
     static constexpr int W_BYTES = RP * 128, W_RAW = FP32 && !WIDE_W ? RP * 64 : W_BYTES, W_MORE = FP32 ? W_BYTES : 0;
     static constexpr int X_PART = X_BYTES * (FP32 ? 2 : 1), STAGE = X_PART + W_RAW + W_MORE;
-    static constexpr int STAGES = FP32 ? 3 : 4;
+    static constexpr int STAGES = TWO ? 2 : FP32 ? 3 : 4;
     static constexpr int CHUNK = FP32 ? 2 : 4;                                      // stages whose products the tensor core adds up
     static constexpr int T_ROW = RP * (BF ? 2 : 4), KB = (T_ROW + 127) / 128;       // bytes of a row of t, and blocks of 128
     static constexpr int T_BYTES = KB * TILE_M * 128;                               // one term
@@ -47,10 +50,10 @@ struct TileLayout {
     static constexpr int T_KEPT = TILE_M * RP * 4;                                  // t in FP32, for the cluster and for odd sums
     static constexpr int W2_BASE = 2 * T_BYTES, KEPT_BASE = W2_BASE + W2_SETS * W2_SET, PHASE2 = KEPT_BASE + T_KEPT;
     static constexpr int WORK = STAGES * STAGE > PHASE2 ? STAGES * STAGE : PHASE2;
-    static constexpr int SLOTS = GROUPS == 2 ? 2 : FP32 ? 1 : 2;                  // of each warp: 32 rows x 128 bytes of base and y
-    static constexpr int SLOT_BASE = WORK, BARS = SLOT_BASE + WORK_WARPS * SLOTS * SLOT_BYTES;
-    static constexpr int SMEM = BARS + 512 + 1024;                                  // barriers, and alignment to 1024
-    static constexpr int TMEM = 256;                                                // 2 x rank columns of t, later 64 of y for each group
+    static constexpr int SLOTS = TWO || (FP32 && GROUPS == 4) ? 1 : 2;                 // of each warp: 32 rows x 128 bytes of base and y
+    static constexpr int SLOT_BASE = WORK, END = SLOT_BASE + WORK_WARPS * SLOTS * SLOT_BYTES;
+    static constexpr int SMEM = END + 1024;                                         // to start at a multiple of 1024; the barriers lie in front or behind
+    static constexpr int TMEM = 64 * GROUPS;                                        // 2 x rank columns of t, later 64 of y for each group
 };
 
 struct TileArgs {
@@ -149,22 +152,22 @@ __device__ __forceinline__ void widen(const uint8_t* from, uint8_t* to, int tid)
         }
     }
 }
-template <typename XT, typename WT, int RP>
-__global__ void __launch_bounds__(TileLayout<XT, WT, RP>::THREADS, 1) adapter_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w1,
+template <typename XT, typename WT, int RP, bool TWO>
+__global__ void __launch_bounds__(TileLayout<XT, WT, RP, TWO>::THREADS, TWO ? 2 : 1) adapter_tile_kernel(const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_w1,
                                                                        const __grid_constant__ CUtensorMap tm_w2, const __grid_constant__ CUtensorMap tm_base,
                                                                        const __grid_constant__ CUtensorMap tm_out, const TileArgs g)
 {
-    using T = TileLayout<XT, WT, RP>;
+    using T = TileLayout<XT, WT, RP, TWO>;
     constexpr bool NATIVE = !T::FP32, F16_2 = T::BF;
     constexpr int STAGES = T::STAGES, CHUNK = T::CHUNK, SLOTS = T::SLOTS, GROUPS = T::GROUPS, WORK_WARPS = T::WORK_WARPS, SHARE = RP / GROUPS, SETS = T::W2_SETS;
     const RowsArgs& a = g.a;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base_addr = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* smem = smem_raw + (base_addr - smem_u32(smem_raw));
-    const uint32_t bars = base_addr + T::BARS;
+    const uint32_t bars = base_addr - smem_u32(smem_raw) >= 512 ? base_addr - 512 : base_addr + T::END;      // 512 bytes
     const uint32_t full = bars, ready = bars + 32, empty = bars + 64, t_full = bars + 96, t_free = bars + 112, t_ready = bars + 128,
                    w_full = bars + 136, w_empty = bars + 168, w_ready = bars + 200, y_full = bars + 232, slot_full = bars + 264;   // slot_full: [warp][SLOTS]
-    volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(smem + T::BARS + 480);
+    volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(smem_raw + (bars + 480 - smem_u32(smem_raw)));
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -633,15 +636,18 @@ bool encode(EncodeTiledFn enc, CUtensorMap* tm, const void* base, int64_t rows, 
 
 int64_t tiles_of(const RowsArgs& a) { return (a.M + TILE_M - 1) / TILE_M + a.S - 1; }
 
-// one block for every SM: two share the columns of a tile where the tiles alone are at most half as many
+// Up to a tile for every SM one block on each, two sharing a tile's columns where the tiles are at most half as many; more tiles: two blocks on
+// each SM, one of which loads while the other stores (65536 rows, 640 -> 2560, BF16, rank 64: 156 us against 167; 8192 rows: 42 against 33).
 int cluster_of(const RowsArgs& a) { return tiles_of(a) <= 74 ? 2 : 1; }
+bool two_on_an_sm(const RowsArgs& a, int x_type) { return tiles_of(a) > 148 && (a.R <= 32 || x_type == FPQ_BF16); }
 
-template <typename XT, typename WT, int RP>
+template <typename XT, typename WT, int RP, bool TWO>
 fpq_status launch_as(const RowsArgs& a, int x_type, int w_type, cudaStream_t st)
 {
-    using T = TileLayout<XT, WT, RP>;
+    using T = TileLayout<XT, WT, RP, TWO>;
     static_assert(T::SMEM <= 232448, "shared memory");
-    static_assert(T::KB * 128 >= T::T_ROW && 2 * RP + 2 * NCOLS <= T::TMEM, "tensor memory");
+    static_assert(2 * RP <= T::TMEM && T::GROUPS * NCOLS <= T::TMEM, "tensor memory");
+    static_assert(!TWO || 2 * (T::SMEM + 1024) <= 233472, "two blocks on an SM");
     EncodeTiledFn enc = tensor_map_encoder();
     TileArgs g;
     g.a = a;
@@ -651,7 +657,7 @@ fpq_status launch_as(const RowsArgs& a, int x_type, int w_type, cudaStream_t st)
         return FPQ_ERR_CUDA;
     static std::atomic<uint64_t> known{0};
     if (dev >= 64 || !(known.load(std::memory_order_relaxed) >> dev & 1)) {
-        if (cudaFuncSetAttribute(adapter_tile_kernel<XT, WT, RP>, cudaFuncAttributeMaxDynamicSharedMemorySize, T::SMEM) != cudaSuccess)
+        if (cudaFuncSetAttribute(adapter_tile_kernel<XT, WT, RP, TWO>, cudaFuncAttributeMaxDynamicSharedMemorySize, T::SMEM) != cudaSuccess)
             return FPQ_ERR_CUDA;
         if (dev < 64)
             known.fetch_or((uint64_t)1 << dev);
@@ -689,7 +695,16 @@ fpq_status launch_as(const RowsArgs& a, int x_type, int w_type, cudaStream_t st)
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, adapter_tile_kernel<XT, WT, RP>, tx, t1, t2, tb, ty, g) == cudaSuccess ? FPQ_OK : FPQ_ERR_CUDA;
+    return cudaLaunchKernelEx(&cfg, adapter_tile_kernel<XT, WT, RP, TWO>, tx, t1, t2, tb, ty, g) == cudaSuccess ? FPQ_OK : FPQ_ERR_CUDA;
+}
+
+template <typename XT, typename WT, int RP>
+fpq_status launch_rank(const RowsArgs& a, int x_type, int w_type, cudaStream_t st)
+{
+    if constexpr (RP <= 32 || std::is_same<XT, __nv_bfloat16>::value)
+        if (two_on_an_sm(a, x_type))
+            return launch_as<XT, WT, RP, true>(a, x_type, w_type, st);
+    return launch_as<XT, WT, RP, false>(a, x_type, w_type, st);
 }
 
 template <typename XT, typename WT>
@@ -699,9 +714,9 @@ fpq_status launch_type(const RowsArgs& a, int x_type, int w_type, cudaStream_t s
         if constexpr (sizeof(XT) == 4)
             return FPQ_ERR_UNSUPPORTED;                    // (adapter_tiles_preferred)
         else
-            return launch_as<XT, WT, 16>(a, x_type, w_type, st);
+            return launch_rank<XT, WT, 16>(a, x_type, w_type, st);
     }
-    return a.R <= 32 ? launch_as<XT, WT, 32>(a, x_type, w_type, st) : launch_as<XT, WT, 64>(a, x_type, w_type, st);
+    return a.R <= 32 ? launch_rank<XT, WT, 32>(a, x_type, w_type, st) : launch_rank<XT, WT, 64>(a, x_type, w_type, st);
 }
 
 // what TMA reads or writes: rows at multiples of 16 bytes
@@ -718,19 +733,21 @@ bool adapter_tiles_preferred(const RowsArgs& a, int x_type, int w_type)
     const int wb = w_type == FPQ_FP32 ? 4 : 2;
     if (!mapped(a.w1, a.ld_w1, wb) || (a.out && !mapped(a.w2, a.ld_w2, wb)) || (int64_t)a.G * std::max<int64_t>(a.R, a.out ? a.D2 : 0) >= ((int64_t)1 << 31))
         return false;
-    // Estimates of both passes in us, fitted to 234 shapes of 1024 to 65536 rows (26 % and 20 % rms; the choice costs 3 % over the better
-    // one, the pass by warps alone 21 %).  This one: a wave of blocks has its own latency and 36 bytes per ns and block; the pass by
-    // warps: so many values a us by type and rank.  (8192 x 640 -> 2560, FP32, rank 16: 46 here, 39 by warps; rank 64: 58 and
-    // 113; 65536 rows, BF16, rank 64: 167 and 345.)  FP32 rows of rank 16 gained nothing.  Requests shorter than two tiles, and clusters of more than two blocks, were slower in every case.
+    // Estimates of both passes in us, fitted to 120 shapes of 8192 to 65536 rows (16 % and 19 % rms; the choice costs 1.3 % over the better
+    // one, the pass by warps alone 46 %).  This one: a wave of blocks has its own latency and 31 bytes per ns and block (19 with two on
+    // an SM); the pass by warps: so many values a us by type and rank.  (8192 x 640 -> 2560, FP32, rank 16: 46 here, 39 by warps;
+    // rank 64: 58 and 98; 65536 rows, BF16, rank 64: 156 and 335.)  FP32 rows of rank 16 gained nothing, requests shorter than two
+    // tiles and clusters of more than two blocks were slower in every case.
     const int64_t tiles = tiles_of(a);
     if (tiles <= 37 || a.M < 256 * (int64_t)a.S || (bytes == 4 && a.R <= 16))
         return false;
+    const bool two = two_on_an_sm(a, x_type);
     const int c = cluster_of(a), kind = (a.R <= 16 ? 0 : a.R <= 32 ? 1 : 2) + (bytes == 4 ? 0 : 3);
     const double values = (double)a.M * ((double)a.D1 + (a.out ? (double)a.D2 * (a.base ? 2 : 1) : 0)), moved = values * bytes;
-    const double blocks = (double)tiles * c, waves = (double)((tiles * c + 147) / 148);
-    const double here = 1.6 + 6.4 * waves + (c > 1 ? 6 : 0) + std::max(moved / 5.3e6, moved / blocks * waves / 36e3);
-    static const double rate[6] = {0, 0.77e6, 0.34e6, 2.04e6, 1.59e6, 0.87e6};
-    return here < 6.2 + std::max(values / rate[kind], moved / 5.3e6);
+    const double blocks = (double)tiles * c, waves = ceil(blocks / (two ? 296 : 148));
+    const double here = 6.5 * waves + (c > 1 ? 2.8 : 0) + std::max(moved / 5.3e6, moved / blocks * waves / (two ? 19.3e3 : 31e3));
+    static const double rate[6] = {0, 0.71e6, 0.37e6, 1.81e6, 1.39e6, 0.81e6};
+    return here < 4.7 + std::max(values / rate[kind], moved / 5.3e6);
 }
 
 fpq_status launch_adapter_tiles(const RowsArgs& a, int x_type, int w_type, cudaStream_t st)

@@ -192,6 +192,9 @@ TALL = [
     (9400, 648, 1288, 24, [0, 4600, 9400], [0, -1], 1),
     (18900, 1288, 648, 16, [3, 18899], [1], 2),
     (18931, 640, 1280, 32, [0, 18931], [0], 1),
+    (21000, 328, 648, 64, [0, 9000, 9000, 20990], [1, 0, 0], 2),
+    (28001, 648, 1288, 16, [0, 14000, 28001], [0, 1], 2),
+    (28000, 1288, 648, 24, [1, 20000, 27999], [1, 0], 2),
     (12000, 64, 1032, 40, [5, 6000, 11990], [0, 1], 2),
 ]
 
@@ -208,10 +211,12 @@ TALL_CASES = [(s, x, w) for s in TALL for x, w in TYPES if any(by_tiles(s, x, w)
 
 def test_tall_requests_reach_their_kernel():
     """Every type and padded rank that the kernel is built for is among the cases, forward and backward."""
-    seen = {(x, w, max(16, 1 << (s[3] - 1).bit_length()), way) for s, x, w in TALL_CASES for way, yes in enumerate(by_tiles(s, x, w)) if yes}
+    seen = {(x, w, max(16, 1 << (s[3] - 1).bit_length()), s[0] > 148 * 128, way)
+            for s, x, w in TALL_CASES for way, yes in enumerate(by_tiles(s, x, w)) if yes}
     for x, w in TYPES:
         for rp in (32, 64) if x == F32 else (16, 32, 64):
-            assert {way for a, b, r, way in seen if (a, b, r) == (x, w, rp)} >= {0, 2}, (x, w, rp)
+            for more_than_sms in (False, True):            # up to a tile for every SM, and more
+                assert {way for *k, way in seen if k == [x, w, rp, more_than_sms]} >= {0, 2}, (x, w, rp, more_than_sms)
     assert not any(by_tiles((8192, 640, 640, 128, [0, 8192], [0], 1), F32, F32))
     with pytest.raises(fpq.FpqError, match="shape"):
         fpq.fpq_adapter_route(1, 1, 1, 1, 200, 1, fpq.FP32, fpq.FP32)
