@@ -435,10 +435,10 @@ fpq_status fpq_round_learn_harden(const float* alpha, int64_t N, int64_t K, uint
  *            out of range); ids [S] int32.  One adapter may serve any number of segments; segments may be empty
  *   u        NULL, or [M][R] FP32 out: what fpq_adapter_backward reads
  * Sums are FP32: FP32 operands enter the tensor cores as two TF32 terms each (errors of 2^-22 of the sum of absolute
- * terms, as FP32 multiply-adds have), 16-bit operands as they are (with BF16, t in two terms: 2^-18 of it is left out); y is
- * rounded once.  An infinite or NaN operand gives
- * what FP32 multiply-adds give.  A row's result depends on its own values and the sizes of the call alone, and equal calls give
- * equal bits.
+ * terms, as FP32 multiply-adds have; the second term of a number below 2^-114 is subnormal and counts as zero: 2^-11 of it can be
+ * lost), 16-bit operands as they are (with BF16, t in two terms: 2^-18 of it is left out); y is rounded once.  An infinite or NaN
+ * operand gives what FP32 multiply-adds give.  A row's result depends on its own values, its adapter, and the sizes and alignment of
+ * the call alone, and equal calls give equal bits.
  *
  * fpq_adapter_backward: the gradients, from dy [M][N] (rows ld_dy apart) and what forward read and kept:
  *     t[i] = scale[g] * B[g]^T dy[i],   dx[i] = base[i] + A[g]^T t[i],
@@ -447,7 +447,8 @@ fpq_status fpq_round_learn_harden(const float* alpha, int64_t N, int64_t K, uint
  *   dx       [M][K] out, or NULL when x needs no gradient; rows in no segment stay as they were
  *   da, db   [G][R][K] and [G][N][R] FP32 out, overwritten (zeros for an adapter without rows).  No atomics: equal calls
  *            give equal bits
- *   workspace  fpq_adapter_backward_workspace_size bytes (0 for sizes out of range), 16-byte aligned, contents not kept
+ *   workspace  fpq_adapter_backward_workspace_size bytes (0 for sizes out of range), 16-byte aligned, contents not kept; not for two
+ *            calls at once
  * One kernel forward, three backward, on `stream`; no allocation, no synchronisation.  Pointers are aligned to their
  * element; rows at multiples of 16 bytes are read 16 bytes at a time.  Limits: M and S below 2^31 and 2^24, N and K
  * up to 2^24, G up to 65535, G * R * max(N, K) below 2^40, G * (N + K) below 2^33.  M = 0 or S = 0: forward does nothing, backward writes zeros to
@@ -493,7 +494,8 @@ fpq_status fpq_adapter_backward(const void* dy, int64_t ld_dy, const void* x, in
  *            half the square root's
  *   options_host  lr, weight_decay finite; beta1, beta2 in [0, 1); eps zero, or a normal positive FP32 number
  *   factors  NULL (ones) or DEVICE float[2]: what a schedule or a gradient clip changes between replays of a captured call
- *   step     DEVICE int64[2] {steps made, 0}, advanced by the call; the second entry is scratch, zero before and after
+ *   step     DEVICE int64[2] {steps made, 0}, advanced by the call; the second entry is scratch, zero before and after.  Calls that
+ *            share it run one after the other (one stream, or streams that wait)
  * One kernel per 400 tensors on `stream`.  Errors: FPQ_ERR_UNSUPPORTED (types), FPQ_ERR_SHAPE (count or n negative, n or
  * their sum not below 2^40, options out of range), FPQ_ERR_NULL, FPQ_ERR_ALIGN (pointers to their element; step 8 bytes),
  * FPQ_ERR_CUDA.

@@ -14,8 +14,8 @@
 // fragments, the sums.  That and the latency of a tile bound it, not the memory.
 //
 // Backward then forms dA and dB (adapter_grad_kernel): columns of x with t and of dy with u, rows split over blocks and added up in a
-// fixed order.  30011 x 1280 -> 640, BF16, rank 32, three adapters: some 45 of 99 us.  Four launches that overlap (weights transposed, rows,
-// gradients, their sums): of a small call's 13 us most is their latency.
+// fixed order.  30011 x 1280 -> 640, BF16, rank 32, three adapters: some 45 of 95 us.  Three launches that overlap (weights transposed, rows,
+// gradients): of a small call's 13 us most is their latency.
 //
 // Products run on the tensor cores as TF32 with FP32 operands in two terms x = hi + lo of 11 significant bits each: hi hi, hi lo and
 // lo hi (16-bit operands are TF32 numbers themselves, one term, or are multiplied as they are).  Some 2^-22 of a product is left
@@ -565,14 +565,16 @@ __global__ void __launch_bounds__(THREADS, RP <= 64 ? 2 : 1) adapter_rows_kernel
 }
 
 // Adapters transposed for the backward pass, 32 x 32 at a time: [G][R][K] to [G][K][ldr] and [G][N][R] to [G][R][ldn], rows of which start
-// at multiples of 16 bytes, zeros behind their ends.
+// at multiples of 16 bytes, zeros behind their ends; and the tickets of the gradients' blocks set to zero.
 template <typename T>
 __global__ void __launch_bounds__(THREADS) transpose_adapters_kernel(const T* a, T* at, const T* b, T* bt, int R, int K, int N, int ldr, int ldn,
-                                                                     int tiles_a, int tiles)
+                                                                     int tiles_a, int tiles, uint32_t* tickets, int n_tickets)
 {
     __shared__ T piece[32][33];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (threadIdx.x == 0 && (int)blockIdx.x < n_tickets)
+        tickets[blockIdx.x] = 0;                           // (there are more blocks than tickets: 32 columns each instead of 64)
     const int g = blockIdx.x / tiles, t = blockIdx.x % tiles;
     const bool is_b = t >= tiles_a;
     const int rows = is_b ? N : R, cols = is_b ? R : K, ld = is_b ? ldn : ldr, across = (cols + 31) / 32, i = is_b ? t - tiles_a : t;
@@ -592,7 +594,8 @@ __global__ void __launch_bounds__(THREADS) transpose_adapters_kernel(const T* a,
 // ---- gradients of the adapters -----------------------------------------------------------------------------------
 // out(col, j) = sum over an adapter's rows of wide[i][col] * thin[i][j]: columns of x with t (dA) and of dy with u (dB).  A
 // block takes 64 columns; its warps, and the blocks with the same columns, share the rows in runs.  Sums are added up in a fixed
-// order: those of the warps in shared memory, those of the blocks by a kernel behind this one.
+// order: those of the warps in shared memory, those of the blocks by the one that is the last of them to end (a kernel of its own
+// behind this one: 2 us more).
 struct GradArgs {
     const void *x, *dy;
     const float *t, *u;            // [M][R]
@@ -603,6 +606,7 @@ struct GradArgs {
     int G, R, S, x_by, dy_by;
     int tiles_k, tiles;            // column tiles of dA; those behind them are dB's
     float* sums;                   // [split][G][tiles][64 RP] where the rows are split
+    uint32_t* tickets;             // [G][tiles]: how many of the blocks that share a sum have ended
     int splits;
 };
 
@@ -625,7 +629,7 @@ __device__ __forceinline__ void store_gradient(const GradArgs& a, int id, bool i
             if (a.ids[sg] != id)
                 continue;
             const int64_t begin = min(max((int64_t)a.offsets[sg], (int64_t)0), a.M), end = min(max((int64_t)a.offsets[sg + 1], (int64_t)0), a.M);
-            for (int64_t r = begin; r < end; ++r)
+            for (int64_t r = begin; r < end && v == v; ++r)    // (a NaN stays one)
                 v = fmaf(as_float(wide[r * ld]), thin[r * a.R], v);
         }
     }
@@ -655,28 +659,6 @@ __device__ __forceinline__ int splits_of(const GradArgs& a, int id)
         mine += __shfl_xor_sync(0xffffffffu, mine, o);
     }
     return all == 0 ? 1 : max((int)((mine * a.splits + all - 1) / all), 1);
-}
-
-template <typename XT>
-__global__ void __launch_bounds__(THREADS) adapter_grad_sum_kernel(const GradArgs a, int RP)
-{
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const int per = 64 * RP / THREADS, tile = blockIdx.x / per, id = blockIdx.y, i = blockIdx.x % per * THREADS + threadIdx.x;
-    const bool is_b = tile >= a.tiles_k;
-    int col, j;
-    tile_element(i, RP, is_b, col, j);
-    col += (is_b ? tile - a.tiles_k : tile) * 64;
-    const int splits = splits_of(a, id);
-    if (splits == 1 || col >= (is_b ? a.N : a.K) || j >= a.R)
-        return;                                            // (with one, the block itself has stored them)
-    const int64_t step = (int64_t)a.G * a.tiles * 64 * RP;
-    const float* s = a.sums + ((int64_t)id * a.tiles + tile) * 64 * RP + i;
-    float v = 0.f;
-#pragma unroll 8
-    for (int z = 0; z < splits; ++z)
-        v += s[z * step];
-    store_gradient<XT>(a, id, is_b, col, j, v);
 }
 
 // Every warp has a ring of its own in shared memory: runs of 16 (32) rows of 64 columns and of its JT ranks, fetched asynchronously
@@ -957,6 +939,36 @@ __global__ void __launch_bounds__(THREADS, 2) adapter_grad_kernel(const GradArgs
         else if (c0 + col < D && j < R)
             store_gradient<XT>(a, id, is_b, c0 + col, j, v);
     }
+    if (splits == 1)
+        return;
+    __shared__ int last;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        uint32_t ended;
+        asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(ended) : "l"(a.tickets + (int64_t)id * a.tiles + tile) : "memory");
+        last = ended == (uint32_t)splits - 1;
+    }
+    __syncthreads();
+    if (!last)
+        return;
+    sums = a.sums + ((int64_t)id * a.tiles + tile) * 64 * RP;
+    const int64_t next = (int64_t)a.G * a.tiles * 64 * RP;
+#pragma unroll 1
+    for (int i = threadIdx.x; i < 64 * RP; i += 4 * THREADS) {
+        float v[4] = {};
+#pragma unroll 4
+        for (int z = 0; z < splits; ++z)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                v[k] += sums[z * next + i + k * THREADS];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            int col, j;
+            tile_element(i + k * THREADS, RP, is_b, col, j);
+            if (c0 + col < D && j < R)
+                store_gradient<XT>(a, id, is_b, c0 + col, j, v[k]);
+        }
+    }
 }
 
 // ---- launches ----------------------------------------------------------------------------------------------------
@@ -1078,10 +1090,7 @@ cudaError_t launch_grad_as(const GradArgs& a, cudaStream_t st)
     using Ring = GradRing<XT, JT>;
     const size_t smem = std::max<size_t>((size_t)(WARPS / (RP / JT)) * 64 * (RP + 2) * 4, (size_t)WARPS * Ring::STAGES * Ring::STAGE);
     static std::atomic<uint64_t> known{0};
-    const cudaError_t e = launch_cluster<GradArgs>(adapter_grad_kernel<XT, RP, JT>, known, (int)smem, dim3(a.tiles, a.G, a.splits), 1, smem, st, a);
-    if (e != cudaSuccess || a.splits == 1)
-        return e;
-    return launch_overlapped(adapter_grad_sum_kernel<XT>, dim3(a.tiles * (64 * RP / THREADS), a.G), THREADS, 0, st, a, RP);
+    return launch_cluster<GradArgs>(adapter_grad_kernel<XT, RP, JT>, known, (int)smem, dim3(a.tiles, a.G, a.splits), 1, smem, st, a);
 }
 
 template <typename XT>
@@ -1098,11 +1107,11 @@ int padded_ranks(int R, int bytes) { return (int)round_up(R, bytes == 4 && R <= 
 int padded_columns(int64_t N, int bytes) { return (int)round_up(N, 16 / bytes); }
 
 template <typename T>
-cudaError_t launch_transpose_as(const AdapterProblem& p, T* at, T* bt, cudaStream_t st)
+cudaError_t launch_transpose_as(const AdapterProblem& p, T* at, T* bt, uint32_t* tickets, int n_tickets, cudaStream_t st)
 {
     const int64_t r = (p.R + 31) / 32, tiles_a = r * ((p.K + 31) / 32), tiles = tiles_a + r * ((p.N + 31) / 32);
     return launch_overlapped(transpose_adapters_kernel<T>, dim3((unsigned)(tiles * p.G)), THREADS, 0, st, (const T*)p.a, at, (const T*)p.b, bt,
-                             p.R, (int)p.K, (int)p.N, padded_ranks(p.R, sizeof(T)), padded_columns(p.N, sizeof(T)), (int)tiles_a, (int)tiles);
+                             p.R, (int)p.K, (int)p.N, padded_ranks(p.R, sizeof(T)), padded_columns(p.N, sizeof(T)), (int)tiles_a, (int)tiles, tickets, n_tickets);
 }
 
 size_t pad16(size_t n) { return (n + 15) / 16 * 16; }
@@ -1133,12 +1142,13 @@ bool adapter_forward_by_tiles(const AdapterProblem& p, bool base)
     return p.M > 0 && p.S > 0 && adapter_tiles_preferred(a, p.x_type, p.w_type);
 }
 
-// workspace: t [M][R] FP32, A and B transposed, the sums of the blocks that share an adapter's rows
+// workspace: t [M][R] FP32, A and B transposed, the tickets and the sums of the blocks that share an adapter's rows
 size_t adapter_backward_bytes(int64_t M, int64_t N, int64_t K, int G, int R, int w_type)
 {
     const size_t wb = type_bytes(w_type), g = (size_t)G * wb;
     const int splits = grad_splits(M, N, K, G);
-    const size_t sums = splits == 1 ? 0 : (size_t)splits * G * (column_tiles(K) + column_tiles(N)) * 64 * padded_rank(R) * 4;
+    const size_t tiles = (size_t)G * (column_tiles(K) + column_tiles(N));
+    const size_t sums = splits == 1 ? 0 : pad16(tiles * 4) + splits * tiles * 64 * padded_rank(R) * 4;
     return pad16((size_t)M * R * 4) + pad16(g * K * padded_ranks(R, (int)wb)) + pad16(g * R * padded_columns(N, (int)wb)) + sums;
 }
 
@@ -1151,10 +1161,12 @@ cudaError_t launch_adapter_backward(const AdapterProblem& p, const void* dy, int
     const int xb = type_bytes(p.x_type);
     uint8_t* at = (uint8_t*)workspace + pad16((size_t)p.M * p.R * 4);
     uint8_t* bt = at + pad16((size_t)p.G * p.K * padded_ranks(p.R, (int)wb) * wb);
-    float* sums = (float*)(bt + pad16((size_t)p.G * p.R * padded_columns(p.N, (int)wb) * wb));
+    uint32_t* tickets = (uint32_t*)(bt + pad16((size_t)p.G * p.R * padded_columns(p.N, (int)wb) * wb));
+    const int splits = p.M > 0 && p.S > 0 ? grad_splits(p.M, p.N, p.K, p.G) : 1, tiles = column_tiles(p.K) + column_tiles(p.N);
+    const int n_tickets = splits > 1 ? p.G * tiles : 0;    // (below 2^27)
     if (p.M > 0 && p.S > 0) {
-        cudaError_t e = wb == 4 ? launch_transpose_as(p, (uint32_t*)at, (uint32_t*)bt, st)
-                                                  : launch_transpose_as(p, (uint16_t*)at, (uint16_t*)bt, st);
+        cudaError_t e = wb == 4 ? launch_transpose_as(p, (uint32_t*)at, (uint32_t*)bt, tickets, n_tickets, st)
+                                : launch_transpose_as(p, (uint16_t*)at, (uint16_t*)bt, tickets, n_tickets, st);
         if (e != cudaSuccess)
             return e;
         RowsArgs a = {};
@@ -1173,9 +1185,10 @@ cudaError_t launch_adapter_backward(const AdapterProblem& p, const void* dy, int
     b.x_by = bytes_at_a_time(x, ldx, p.K, xb);
     b.dy_by = bytes_at_a_time(dy, ld_dy, p.N, xb);
     b.tiles_k = column_tiles(p.K);
-    b.tiles = b.tiles_k + column_tiles(p.N);
-    b.sums = sums;
-    b.splits = b.S > 0 ? grad_splits(p.M, p.N, p.K, p.G) : 1;
+    b.tiles = tiles;
+    b.tickets = tickets;
+    b.sums = (float*)((uint8_t*)tickets + pad16((size_t)n_tickets * 4));
+    b.splits = splits;
     return p.x_type == FPQ_FP32 ? launch_grad<float>(b, st) : p.x_type == FPQ_BF16 ? launch_grad<__nv_bfloat16>(b, st) : launch_grad<__half>(b, st);
 }
 

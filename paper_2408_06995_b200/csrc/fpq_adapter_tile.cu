@@ -562,16 +562,19 @@ __global__ void __launch_bounds__(TileLayout<XT, WT, RP, TWO>::THREADS, TWO ? 2 
                     }
                 }
                 if ((zero[0] + zero[1]) + (zero[2] + zero[3]) != 0.f && row < tr.rows) {
-                    // the row again by multiply-adds
+                    // what is not finite again by multiply-adds
                     const float* t = reinterpret_cast<const float*>(smem + T::KEPT_BASE) + row * RP;
                     const XT* b = based ? (const XT*)a.base + (tr.row + row) * a.ld_base + col : nullptr;
 #pragma unroll 1
                     for (int i = 0; i < min(COLS, D2 - col); ++i) {
+                        XT& y = reinterpret_cast<XT*>(sl + swizzled(lane, i / PER))[i % PER];
+                        if (finite(as_float(y)))
+                            continue;
                         float v = 0.f;
 #pragma unroll 1
                         for (int k = 0; k < R; ++k)
                             v = fmaf(t[k], as_float(w2[(col + i) * a.ld_w2 + k]), v);
-                        reinterpret_cast<XT*>(sl + swizzled(lane, i / PER))[i % PER] = from_float<XT>((b ? as_float(b[i]) : 0.f) + v);
+                        y = from_float<XT>((b ? as_float(b[i]) : 0.f) + v);
                     }
                 }
                 if (rows_here >= 32) {

@@ -526,6 +526,37 @@ def test_equal_calls_give_equal_bits_on_two_streams():
 
 
 @pytest.mark.gpu
+def test_workspaces_hold_nothing_between_calls():
+    # many blocks share each sum: whatever the workspace holds, and after a call of other sizes in it, the bits are the same
+    t, other = make(4000, 640, 320, 24, [0, 1500, 4000], [1, 0], 2), make(900, 96, 200, 8, [0, 900], [0], 1)
+    u, v = torch.randn(4000, 24, device="cuda"), torch.randn(900, 8, device="cuda")
+    work = torch.empty(fpq.fpq_adapter_backward_workspace_size(4000, 320, 640, 2, 24, fpq.FP32), dtype=torch.uint8, device="cuda")
+    want = None
+    for fill in (0, 255, 1):
+        work.fill_(fill)
+        for _ in range(2):
+            got = fpq.fpq_adapter_backward(t["dy"], t["x"], u, t["a"], t["b"], t["offsets"], t["ids"], t["scale"], workspace=work)
+            want = want or got
+            assert all(torch.equal(a, b) for a, b in zip(got, want))
+            fpq.fpq_adapter_backward(other["dy"], other["x"], v, other["a"], other["b"], other["offsets"], other["ids"], workspace=work)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("xt", [F32, BF])
+def test_another_adapters_values_change_no_bit(xt):
+    # the last 64 columns of adapter 0 reach into adapter 1's rows of B, its last ranks into those of A: infinite ones may not change how
+    # its own rows are worked out
+    t = make(21000, 648, 328, 40, [0, 20000, 21000], [0, 1], 2, xt, xt)
+    assert fpq.fpq_adapter_route(21000, 328, 648, 2, 40, 2, fpq._REAL[xt], fpq._REAL[xt]) == fpq.ADAPTER_TILES
+    _, y, u = run_forward(t)
+    t["b"][1] = float("inf")
+    t["a"][1] = float("nan")
+    _, z, v = run_forward(t)
+    assert torch.equal(y[:20000], z[:20000]) and torch.equal(u[:20000], v[:20000])
+    assert not bool(torch.isfinite(z[20000:]).any())
+
+
+@pytest.mark.gpu
 def test_binding_refuses():
     t = make(10, 32, 16, 4, [0, 10], [0], 1)
     ok = [t["x"], t["a"], t["b"], t["offsets"], t["ids"], t["scale"], t["base"], torch.zeros(10, 16, device="cuda"), None]
