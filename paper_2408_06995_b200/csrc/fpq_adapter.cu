@@ -596,69 +596,11 @@ __global__ void __launch_bounds__(THREADS) transpose_adapters_kernel(const T* a,
 // block takes 64 columns; its warps, and the blocks with the same columns, share the rows in runs.  Sums are added up in a fixed
 // order: those of the warps in shared memory, those of the blocks by the one that is the last of them to end (a kernel of its own
 // behind this one: 2 us more).
-struct GradArgs {
-    const void *x, *dy;
-    const float *t, *u;            // [M][R]
-    const float* scale;
-    const int32_t *offsets, *ids;
-    float *da, *db;                // [G][R][K], [G][N][R]
-    int64_t M, N, K, ldx, ld_dy;
-    int G, R, S, x_by, dy_by;
-    int tiles_k, tiles;            // column tiles of dA; those behind them are dB's
-    float* sums;                   // [split][G][tiles][64 RP] where the rows are split
-    uint32_t* tickets;             // [G][tiles]: how many of the blocks that share a sum have ended
-    int splits;
-};
-
 // Element i of a tile's 64 RP, in the order of the output's contiguous side.
 __device__ __forceinline__ void tile_element(int i, int RP, bool is_b, int& col, int& j)
 {
     col = is_b ? i / RP : i % 64;
     j = is_b ? i % RP : i / 64;
-}
-
-template <typename XT>
-__device__ __forceinline__ void store_gradient(const GradArgs& a, int id, bool is_b, int64_t col, int j, float v)
-{
-    if (!finite(v)) {
-        const XT* wide = (const XT*)(is_b ? a.dy : a.x) + col;
-        const float* thin = (is_b ? a.u : a.t) + j;
-        const int64_t ld = is_b ? a.ld_dy : a.ldx;
-        v = 0.f;
-        for (int sg = 0; sg < a.S; ++sg) {
-            if (a.ids[sg] != id)
-                continue;
-            const int64_t begin = min(max((int64_t)a.offsets[sg], (int64_t)0), a.M), end = min(max((int64_t)a.offsets[sg + 1], (int64_t)0), a.M);
-            for (int64_t r = begin; r < end && v == v; ++r)    // (a NaN stays one)
-                v = fmaf(as_float(wide[r * ld]), thin[r * a.R], v);
-        }
-    }
-    if (is_b)
-        a.db[((int64_t)id * a.N + col) * a.R + j] = a.scale ? v * a.scale[id] : v;
-    else
-        a.da[((int64_t)id * a.R + j) * a.K + col] = v;
-}
-
-// Over how many of the a.splits blocks adapter `id`'s rows are spread: its share of all rows, so that adapters of unequal length end together.
-// Called by whole warps.
-__device__ __forceinline__ int splits_of(const GradArgs& a, int id)
-{
-    if (a.splits == 1 || a.G == 1)
-        return a.splits;
-    int64_t mine = 0, all = 0;
-    for (int sg = threadIdx.x & 31; sg < a.S; sg += 32) {
-        const int other = a.ids[sg], n = min(max(a.offsets[sg + 1], 0), (int)a.M) - min(max(a.offsets[sg], 0), (int)a.M);
-        if (n > 0 && other >= 0 && other < a.G) {
-            all += n;
-            mine += other == id ? n : 0;
-        }
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) {
-        all += __shfl_xor_sync(0xffffffffu, all, o);
-        mine += __shfl_xor_sync(0xffffffffu, mine, o);
-    }
-    return all == 0 ? 1 : max((int)((mine * a.splits + all - 1) / all), 1);
 }
 
 // Every warp has a ring of its own in shared memory: runs of 16 (32) rows of 64 columns and of its JT ranks, fetched asynchronously
@@ -1146,9 +1088,11 @@ bool adapter_forward_by_tiles(const AdapterProblem& p, bool base)
 size_t adapter_backward_bytes(int64_t M, int64_t N, int64_t K, int G, int R, int w_type)
 {
     const size_t wb = type_bytes(w_type), g = (size_t)G * wb;
-    const int splits = grad_splits(M, N, K, G);
-    const size_t tiles = (size_t)G * (column_tiles(K) + column_tiles(N));
-    const size_t sums = splits == 1 ? 0 : pad16(tiles * 4) + splits * tiles * 64 * padded_rank(R) * 4;
+    const size_t splits = grad_splits(M, N, K, G), tiles = (size_t)G * (column_tiles(K) + column_tiles(N));
+    size_t blocks = splits == 1 ? 0 : splits * tiles * 64;
+    if (w_type == FPQ_BF16)                                // (of rows in BF16, or in FP32)
+        blocks = std::max(blocks, adapter_grad_tile_columns(M, N, K, G, R));
+    const size_t sums = blocks == 0 ? 0 : pad16(tiles * 4) + blocks * padded_rank(R) * 4;
     return pad16((size_t)M * R * 4) + pad16(g * K * padded_ranks(R, (int)wb)) + pad16(g * R * padded_columns(N, (int)wb)) + sums;
 }
 
@@ -1162,8 +1106,18 @@ cudaError_t launch_adapter_backward(const AdapterProblem& p, const void* dy, int
     uint8_t* at = (uint8_t*)workspace + pad16((size_t)p.M * p.R * 4);
     uint8_t* bt = at + pad16((size_t)p.G * p.K * padded_ranks(p.R, (int)wb) * wb);
     uint32_t* tickets = (uint32_t*)(bt + pad16((size_t)p.G * p.R * padded_columns(p.N, (int)wb) * wb));
-    const int splits = p.M > 0 && p.S > 0 ? grad_splits(p.M, p.N, p.K, p.G) : 1, tiles = column_tiles(p.K) + column_tiles(p.N);
-    const int n_tickets = splits > 1 ? p.G * tiles : 0;    // (below 2^27)
+    GradArgs b = {};
+    b.x = x; b.dy = dy; b.t = t; b.u = u; b.scale = p.scale; b.offsets = p.offsets; b.ids = p.ids; b.da = da; b.db = db;
+    b.M = p.M; b.N = p.N; b.K = p.K; b.ldx = ldx; b.ld_dy = ld_dy; b.G = p.G; b.R = p.R; b.S = p.M > 0 ? p.S : 0;
+    b.x_by = bytes_at_a_time(x, ldx, p.K, xb);
+    b.dy_by = bytes_at_a_time(dy, ld_dy, p.N, xb);
+    b.tiles_k = column_tiles(p.K);
+    b.tiles = b.tiles_k + column_tiles(p.N);
+    b.tickets = tickets;
+    const bool by_tiles = b.S > 0 && p.x_type == FPQ_BF16 && adapter_grad_tiles_preferred(b);
+    b.splits = b.S == 0 ? 1 : by_tiles ? adapter_grad_tile_splits(p.M, p.N, p.K, p.G, p.R) : grad_splits(p.M, p.N, p.K, p.G);
+    const int n_tickets = b.splits > 1 ? p.G * b.tiles : 0;    // (below 2^27)
+    b.sums = (float*)((uint8_t*)tickets + pad16((size_t)n_tickets * 4));
     if (p.M > 0 && p.S > 0) {
         cudaError_t e = wb == 4 ? launch_transpose_as(p, (uint32_t*)at, (uint32_t*)bt, tickets, n_tickets, st)
                                 : launch_transpose_as(p, (uint16_t*)at, (uint16_t*)bt, tickets, n_tickets, st);
@@ -1179,16 +1133,8 @@ cudaError_t launch_adapter_backward(const AdapterProblem& p, const void* dy, int
         if (e != cudaSuccess)
             return e;
     }
-    GradArgs b = {};
-    b.x = x; b.dy = dy; b.t = t; b.u = u; b.scale = p.scale; b.offsets = p.offsets; b.ids = p.ids; b.da = da; b.db = db;
-    b.M = p.M; b.N = p.N; b.K = p.K; b.ldx = ldx; b.ld_dy = ld_dy; b.G = p.G; b.R = p.R; b.S = p.M > 0 ? p.S : 0;
-    b.x_by = bytes_at_a_time(x, ldx, p.K, xb);
-    b.dy_by = bytes_at_a_time(dy, ld_dy, p.N, xb);
-    b.tiles_k = column_tiles(p.K);
-    b.tiles = tiles;
-    b.tickets = tickets;
-    b.sums = (float*)((uint8_t*)tickets + pad16((size_t)n_tickets * 4));
-    b.splits = splits;
+    if (by_tiles)
+        return launch_adapter_grad_tiles(b, st);
     return p.x_type == FPQ_FP32 ? launch_grad<float>(b, st) : p.x_type == FPQ_BF16 ? launch_grad<__nv_bfloat16>(b, st) : launch_grad<__half>(b, st);
 }
 

@@ -5,7 +5,9 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include "fpq_common.cuh"
 #include "fpq_kernels.h"
+#include "fpq_tensormap.h"
 
 namespace fpq {
 
@@ -179,5 +181,113 @@ struct RowsArgs {
 // the one by warps, and its launch.
 bool adapter_tiles_preferred(const RowsArgs& a, int x_type, int w_type);
 fpq_status launch_adapter_tiles(const RowsArgs& a, int x_type, int w_type, cudaStream_t st);
+
+// ---- gradients ---------------------------------------------------------------------------------------------------
+struct GradArgs {
+    const void *x, *dy;
+    const float *t, *u;            // [M][R]
+    const float* scale;
+    const int32_t *offsets, *ids;
+    float *da, *db;                // [G][R][K], [G][N][R]
+    int64_t M, N, K, ldx, ld_dy;
+    int G, R, S, x_by, dy_by;
+    int tiles_k, tiles;            // column tiles of dA; those behind them are dB's
+    float* sums;                   // [split][G][tiles][64 RP] where the rows are split
+    uint32_t* tickets;             // [G][tiles]: how many of the blocks that share a sum have ended
+    int splits;
+};
+
+template <typename XT>
+__device__ __forceinline__ void store_gradient(const GradArgs& a, int id, bool is_b, int64_t col, int j, float v)
+{
+    if (!finite(v)) {
+        const XT* wide = (const XT*)(is_b ? a.dy : a.x) + col;
+        const float* thin = (is_b ? a.u : a.t) + j;
+        const int64_t ld = is_b ? a.ld_dy : a.ldx;
+        v = 0.f;
+        for (int sg = 0; sg < a.S; ++sg) {
+            if (a.ids[sg] != id)
+                continue;
+            const int64_t begin = min(max((int64_t)a.offsets[sg], (int64_t)0), a.M), end = min(max((int64_t)a.offsets[sg + 1], (int64_t)0), a.M);
+            for (int64_t r = begin; r < end && v == v; ++r)    // (a NaN stays one)
+                v = fmaf(as_float(wide[r * ld]), thin[r * a.R], v);
+        }
+    }
+    if (is_b)
+        a.db[((int64_t)id * a.N + col) * a.R + j] = a.scale ? v * a.scale[id] : v;
+    else
+        a.da[((int64_t)id * a.R + j) * a.K + col] = v;
+}
+
+// Over how many of the a.splits blocks adapter `id`'s rows are spread: its share of all rows, so that adapters of unequal length end together.
+// Called by whole warps.
+__device__ __forceinline__ int splits_of(const GradArgs& a, int id)
+{
+    if (a.splits == 1 || a.G == 1)
+        return a.splits;
+    int64_t mine = 0, all = 0;
+    for (int sg = threadIdx.x & 31; sg < a.S; sg += 32) {
+        const int other = a.ids[sg], n = min(max(a.offsets[sg + 1], 0), (int)a.M) - min(max(a.offsets[sg], 0), (int)a.M);
+        if (n > 0 && other >= 0 && other < a.G) {
+            all += n;
+            mine += other == id ? n : 0;
+        }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        all += __shfl_xor_sync(0xffffffffu, all, o);
+        mine += __shfl_xor_sync(0xffffffffu, mine, o);
+    }
+    return all == 0 ? 1 : max((int)((mine * a.splits + all - 1) / all), 1);
+}
+
+// The gradients by tcgen05 MMAs, for BF16 rows (fpq_adapter_grad_tile.cu): whether it applies and is expected to be faster, over how many
+// blocks the rows are split, how many columns of sums that takes (0: none), and the launch (a.splits is set).
+bool adapter_grad_tiles_preferred(const GradArgs& a);
+int adapter_grad_tile_splits(int64_t M, int64_t N, int64_t K, int G, int R);
+size_t adapter_grad_tile_columns(int64_t M, int64_t N, int64_t K, int G, int R);
+cudaError_t launch_adapter_grad_tiles(GradArgs a, cudaStream_t st);
+
+// what TMA reads or writes: rows at multiples of 16 bytes
+inline bool mapped(const void* p, int64_t ld, int bytes) { return (uintptr_t)p % 16 == 0 && ld * bytes % 16 == 0 && ld * bytes < ((int64_t)1 << 40); }
+// rows x cols of a type (FPQ_FP32, ...), rows ld elements apart: boxes of box_rows x box_cols, zeros outside; 128-byte swizzle for boxes
+// of 128 bytes
+bool encode_rows(EncodeTiledFn enc, CUtensorMap* tm, const void* base, int64_t rows, int64_t cols, int64_t ld, int type, int box_rows, int box_cols,
+                 bool swizzle);
+
+__device__ __forceinline__ void tma_load_2d(uint32_t dst, const void* tmap, uint32_t bar, int c0, int c1)
+{
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+                 ::"r"(dst), "l"(tmap), "r"(bar), "r"(c0), "r"(c1)
+                 : "memory");
+}
+
+// N consecutive FP32 columns of this thread's lane of tensor memory (not waited for)
+template <int N>
+__device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t* r)
+{
+    if constexpr (N == 32) {
+        tmem_ld32(addr, r);
+    } else if constexpr (N == 16) {
+        asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                     : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+                       "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                     : "r"(addr)
+                     : "memory");
+    } else if constexpr (N == 4) {
+        asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+                     : "r"(addr)
+                     : "memory");
+    } else {
+        asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+                     : "r"(addr)
+                     : "memory");
+    }
+}
+
+// 16-byte piece c of row r of an operand tile: rows of 128 bytes, 128-byte swizzle
+__device__ __forceinline__ int swizzled(int r, int c) { return r * 128 + ((c ^ (r & 7)) << 4); }
 
 }  // namespace fpq

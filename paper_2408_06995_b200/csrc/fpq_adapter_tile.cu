@@ -16,11 +16,9 @@
 
 #include <algorithm>
 #include <atomic>
-#include <mutex>
 #include <type_traits>
 
 #include "fpq_adapter.cuh"
-#include "fpq_tensormap.h"
 
 namespace fpq {
 
@@ -62,12 +60,6 @@ struct TileArgs {
     uint32_t idesc1, idesc2;
 };
 
-__device__ __forceinline__ void tma_load_2d(uint32_t dst, const void* tmap, uint32_t bar, int c0, int c1)
-{
-    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
-                 ::"r"(dst), "l"(tmap), "r"(bar), "r"(c0), "r"(c1)
-                 : "memory");
-}
 __device__ __forceinline__ void tma_store_2d(const void* tmap, uint32_t src, int c0, int c1)
 {
     asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];"
@@ -91,36 +83,8 @@ __device__ __forceinline__ void mma_tile(uint32_t d, uint32_t a_lo, uint32_t b_l
                      : "memory");
 }
 
-// N consecutive FP32 columns of this thread's lane of tensor memory (not waited for)
-template <int N>
-__device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t* r)
-{
-    if constexpr (N == 32) {
-        tmem_ld32(addr, r);
-    } else if constexpr (N == 16) {
-        asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-                     : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
-                       "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-                     : "r"(addr)
-                     : "memory");
-    } else if constexpr (N == 4) {
-        asm volatile("tcgen05.ld.sync.aligned.32x32b.x4.b32 {%0, %1, %2, %3}, [%4];"
-                     : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
-                     : "r"(addr)
-                     : "memory");
-    } else {
-        asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
-                     : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
-                     : "r"(addr)
-                     : "memory");
-    }
-}
-
 // what an FP32 number loses when the tensor core reads it as TF32 (the low 13 mantissa bits are ignored): exact
 __device__ __forceinline__ float tail(float x) { return x - __uint_as_float(__float_as_uint(x) & 0xffffe000u); }
-
-// 16-byte piece c of row r of an operand tile: rows of 128 bytes, 128-byte swizzle
-__device__ __forceinline__ int swizzled(int r, int c) { return r * 128 + ((c ^ (r & 7)) << 4); }
 
 // N 16-byte pieces of FP32 numbers and, at the same places, what TF32 leaves off of them
 template <int N, int THREADS_>
@@ -623,20 +587,6 @@ __global__ void __launch_bounds__(TileLayout<XT, WT, RP, TWO>::THREADS, TWO ? 2 
     }
 }
 
-// rows x cols of a type, rows ld elements apart: boxes of box_rows x box_cols, zeros outside; 128-byte swizzle for boxes of 128 bytes
-bool encode(EncodeTiledFn enc, CUtensorMap* tm, const void* base, int64_t rows, int64_t cols, int64_t ld, int type, int box_rows, int box_cols, bool swizzle)
-{
-    const int bytes = type == FPQ_FP32 ? 4 : 2;
-    const CUtensorMapDataType t = type == FPQ_FP32   ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
-                                  : type == FPQ_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
-                                                     : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
-    cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld * bytes};
-    cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows}, estr[2] = {1, 1};
-    return enc(tm, t, 2, (void*)base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-               swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
 int64_t tiles_of(const RowsArgs& a) { return (a.M + TILE_M - 1) / TILE_M + a.S - 1; }
 
 // Up to a tile for every SM one block on each, two sharing a tile's columns where the tiles are at most half as many; more tiles: two blocks on
@@ -670,13 +620,13 @@ fpq_status launch_as(const RowsArgs& a, int x_type, int w_type, cudaStream_t st)
     const int64_t width = a.out ? a.D2 : a.D1, ld = a.out ? a.ld_out : a.ld_in;
     const int xe = 128 / (int)sizeof(XT);
     const bool raw1 = T::FP32 && !T::WIDE_W, raw2 = !T::BF && !T::WIDE_W;
-    if (!encode(enc, &tx, a.in, a.M, a.D1, a.ld_in, x_type, TILE_M, xe, true) || !encode(enc, &ty, out, a.M, width, ld, x_type, 32, xe, true) ||
-        !encode(enc, &tb, a.out && a.base ? a.base : out, a.M, width, a.out && a.base ? a.ld_base : ld, x_type, 32, xe, true) ||
-        !encode(enc, &t1, a.w1, (int64_t)a.G * a.R, a.D1, a.ld_w1, w_type, RP, raw1 ? 32 : xe, !raw1))
+    if (!encode_rows(enc, &tx, a.in, a.M, a.D1, a.ld_in, x_type, TILE_M, xe, true) || !encode_rows(enc, &ty, out, a.M, width, ld, x_type, 32, xe, true) ||
+        !encode_rows(enc, &tb, a.out && a.base ? a.base : out, a.M, width, a.out && a.base ? a.ld_base : ld, x_type, 32, xe, true) ||
+        !encode_rows(enc, &t1, a.w1, (int64_t)a.G * a.R, a.D1, a.ld_w1, w_type, RP, raw1 ? 32 : xe, !raw1))
         return FPQ_ERR_CUDA;
     if (!a.out)
         t2 = t1;
-    else if (!encode(enc, &t2, a.w2, (int64_t)a.G * a.D2, a.R, a.ld_w2, w_type, NCOLS, raw2 ? RP : 128 / (int)sizeof(WT), !raw2))
+    else if (!encode_rows(enc, &t2, a.w2, (int64_t)a.G * a.D2, a.R, a.ld_w2, w_type, NCOLS, raw2 ? RP : 128 / (int)sizeof(WT), !raw2))
         return FPQ_ERR_CUDA;
     // FP32 accumulators; operands BF16 (1), FP16 (0) or TF32 (2), K-major; M = 128, N = the rank, or 64 columns
     const uint32_t f1 = x_type == FPQ_FP32 ? 2 : x_type == FPQ_BF16 ? 1 : 0, f2 = T::BF ? 1 : 2;
@@ -722,10 +672,21 @@ fpq_status launch_type(const RowsArgs& a, int x_type, int w_type, cudaStream_t s
     return a.R <= 32 ? launch_rank<XT, WT, 32>(a, x_type, w_type, st) : launch_rank<XT, WT, 64>(a, x_type, w_type, st);
 }
 
-// what TMA reads or writes: rows at multiples of 16 bytes
-bool mapped(const void* p, int64_t ld, int bytes) { return (uintptr_t)p % 16 == 0 && ld * bytes % 16 == 0 && ld * bytes < ((int64_t)1 << 40); }
-
 }  // namespace
+
+bool encode_rows(EncodeTiledFn enc, CUtensorMap* tm, const void* base, int64_t rows, int64_t cols, int64_t ld, int type, int box_rows, int box_cols,
+                 bool swizzle)
+{
+    const int bytes = type == FPQ_FP32 ? 4 : 2;
+    const CUtensorMapDataType t = type == FPQ_FP32   ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                  : type == FPQ_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                                     : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld * bytes};
+    cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows}, estr[2] = {1, 1};
+    return enc(tm, t, 2, (void*)base, dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+               swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
 
 bool adapter_tiles_preferred(const RowsArgs& a, int x_type, int w_type)
 {

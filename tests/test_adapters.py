@@ -525,6 +525,56 @@ def test_equal_calls_give_equal_bits_on_two_streams():
         assert all(torch.equal(a, b) for a, b in zip(g, want))
 
 
+GRAD_TILES = [  # M, K, N, R, cuts, ids, G: BF16 rows whose gradients come from tcgen05 tiles of 128 columns and runs of 64 rows
+    (2048, 128, 64, 16, [0, 2048], [0], 1),
+    (2100, 8, 16, 4, [0, 63, 127, 128, 2100], [0, 1, 0, 0], 2),
+    (2777, 200, 328, 32, [3, 70, 70, 1000, 2769], [1, 0, 2, 4], 5),
+    (4099, 320, 136, 12, list(range(0, 4100, 41)), [i % 3 for i in range(99)], 3),
+    (3001, 648, 264, 20, [0, 1, 2, 66, 3001], [0, 1, 1, 0], 2),
+    (5000, 136, 520, 64, [0, 2500, 4990], [1, 0], 2),
+    (2050, 1288, 72, 40, [0, 1025, 2050], [-1, 0], 1),
+    (30000, 64, 64, 8, [0, 29000, 30000], [0, 1], 2),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("shape", GRAD_TILES, ids=lambda s: "x".join(map(str, s[:4])))
+def test_gradients_by_tiles(shape):
+    M, K, N, R, cuts, ids, G = shape
+    t = make(M, K, N, R, cuts, ids, G, BF, BF)
+    outside = torch.ones(M, dtype=torch.bool, device="cuda")
+    for lo, hi, i in segments(t):
+        outside[lo:hi] = i < 0
+    u = torch.randn(M, R, device="cuda")
+    for v in (t["x"], t["dy"], u):                         # rows of no adapter hold what they like
+        v[outside] = float("nan")
+    t["dbase"][outside] = 0
+    dx = torch.zeros_like(t["x"])
+    got = fpq.fpq_adapter_backward(t["dy"], t["x"], u, t["a"], t["b"], t["offsets"], t["ids"], t["scale"], None, dx)
+    check_backward(t, u, *got, torch.zeros_like(dx), base=False)
+    again = fpq.fpq_adapter_backward(t["dy"], t["x"], u, t["a"], t["b"], t["offsets"], t["ids"], t["scale"], need_dx=False)
+    assert torch.equal(got[1], again[1]) and torch.equal(got[2], again[2])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("value", [float("inf"), float("nan"), 3.3e38])
+def test_gradients_by_tiles_of_values_that_are_not_finite(value):
+    t = make(2200, 136, 72, 16, [0, 1000, 2200], [0, 1], 2, BF, BF)
+    u = torch.randn(2200, 16, device="cuda")
+    t["x"][500, 3] = value
+    t["x"][600, 3] = -1.0
+    t["dy"][1500, 5] = value
+    u[700, 2] = value
+    _, da, db = fpq.fpq_adapter_backward(t["dy"], t["x"], u, t["a"], t["b"], t["offsets"], t["ids"], t["scale"], need_dx=False)
+    for i, (lo, hi) in enumerate(((0, 1000), (1000, 2200))):
+        dy, x, s = t["dy"][lo:hi].float(), t["x"][lo:hi].float(), float(t["scale"][i])
+        ea, eb = (s * (dy.double() @ t["b"][i].double())).T @ x.double(), s * (dy.double().T @ u[lo:hi].double())
+        for got, want in ((da[i], ea), (db[i], eb)):
+            fits = want.abs() < 3.0e38                     # (NaN and infinities are not; in between, FP32 sums may run over)
+            assert bool(torch.isfinite(got[fits & (want.abs() < 1e37)]).all())
+            assert not bool(torch.isfinite(got[~(want.abs() <= 3.5e38)]).any())
+
+
 @pytest.mark.gpu
 def test_workspaces_hold_nothing_between_calls():
     # many blocks share each sum: whatever the workspace holds, and after a call of other sizes in it, the bits are the same
