@@ -449,7 +449,7 @@ fpq_status fpq_round_learn_harden(const float* alpha, int64_t N, int64_t K, uint
  *            give equal bits
  *   workspace  fpq_adapter_backward_workspace_size bytes (0 for sizes out of range), 16-byte aligned, contents not kept; not for two
  *            calls at once
- * One kernel forward, three backward, on `stream`; no allocation, no synchronisation.  Pointers are aligned to their
+ * One kernel forward, three or four backward, on `stream`; no allocation, no synchronisation.  Pointers are aligned to their
  * element; rows at multiples of 16 bytes are read 16 bytes at a time.  Limits: M and S below 2^31 and 2^24, N and K
  * up to 2^24, G up to 65535, G * R * max(N, K) below 2^40, G * (N + K) below 2^33.  M = 0 or S = 0: forward does nothing, backward writes zeros to
  * da and db.  Errors: FPQ_ERR_UNSUPPORTED, FPQ_ERR_SHAPE, FPQ_ERR_NULL, FPQ_ERR_ALIGN, FPQ_ERR_WORKSPACE, FPQ_ERR_CUDA.

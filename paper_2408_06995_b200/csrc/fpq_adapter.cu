@@ -13,9 +13,9 @@
 // 300 instructions on 16 x 32 values (half of the issue slots with 16 warps on an SM): operand splits, the addresses of the weights'
 // fragments, the sums.  That and the latency of a tile bound it, not the memory.
 //
-// Backward then forms dA and dB (adapter_grad_kernel): columns of x with t and of dy with u, rows split over blocks and added up in a
-// fixed order.  30011 x 1280 -> 640, BF16, rank 32, three adapters: some 45 of 95 us.  Three launches that overlap (weights transposed, rows,
-// gradients): of a small call's 13 us most is their latency.
+// Backward then forms dA and dB (adapter_grad_kernel; from BF16 rows, by tcgen05 MMAs, fpq_adapter_grad_tile.cu): columns of x with t and of
+// dy with u, rows split over blocks and added up in a fixed order.  8192 x 640 -> 640, FP32, rank 16: 13 of 38 us.  Three launches that
+// overlap (weights transposed, rows, gradients): of a small call's 13 us most is their latency.
 //
 // Products run on the tensor cores as TF32 with FP32 operands in two terms x = hi + lo of 11 significant bits each: hi hi, hi lo and
 // lo hi (16-bit operands are TF32 numbers themselves, one term, or are multiplied as they are).  Some 2^-22 of a product is left
@@ -595,7 +595,7 @@ __global__ void __launch_bounds__(THREADS) transpose_adapters_kernel(const T* a,
 // out(col, j) = sum over an adapter's rows of wide[i][col] * thin[i][j]: columns of x with t (dA) and of dy with u (dB).  A
 // block takes 64 columns; its warps, and the blocks with the same columns, share the rows in runs.  Sums are added up in a fixed
 // order: those of the warps in shared memory, those of the blocks by the one that is the last of them to end (a kernel of its own
-// behind this one: 2 us more).
+// behind this one: 2 us more, 8192 x 640 -> 640).
 // Element i of a tile's 64 RP, in the order of the output's contiguous side.
 __device__ __forceinline__ void tile_element(int i, int RP, bool is_b, int& col, int& j)
 {
@@ -627,15 +627,16 @@ __global__ void __launch_bounds__(THREADS, 2) adapter_grad_kernel(const GradArgs
     float* parts = reinterpret_cast<float*>(smem4);        // at the end: [WK][64][PITCH]
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const int tile = blockIdx.x, id = blockIdx.y;
+    const GradShare share = share_of(a);
+    if (share.z < 0)
+        return;
+    const int tile = blockIdx.x, id = share.id, splits = share.splits;
     const bool is_b = tile >= a.tiles_k;
     const int64_t D = is_b ? a.N : a.K, ld = is_b ? a.ld_dy : a.ldx, c0 = (int64_t)(is_b ? tile - a.tiles_k : tile) * 64;
     const XT* wide = (const XT*)(is_b ? a.dy : a.x);
     const float* thin = is_b ? a.u : a.t;
     const int R = a.R, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
-    const int wn = warp % WN, wk = warp / WN, splits = splits_of(a, id), workers = WK * splits, worker = (int)blockIdx.z * WK + wk, j0 = wn * JT;
-    if ((int)blockIdx.z >= splits)
-        return;
+    const int wn = warp % WN, wk = warp / WN, workers = WK * splits, worker = share.z * WK + wk, j0 = wn * JT;
     uint8_t* ring = reinterpret_cast<uint8_t*>(smem4) + warp * (STAGES * Ring::STAGE);
 
     // the runs of this warp, in order: every workers-th of all runs of the adapter's segments
@@ -868,7 +869,7 @@ __global__ void __launch_bounds__(THREADS, 2) adapter_grad_kernel(const GradArgs
                 *reinterpret_cast<float2*>(parts + (wk * 64 + col) * PITCH + j0 + n * 8 + 2 * q) = make_float2(acc[m][n][2 * h], acc[m][n][2 * h + 1]);
             }
     __syncthreads();
-    float* sums = a.sums + (((int64_t)blockIdx.z * a.G + id) * a.tiles + tile) * 64 * RP;
+    float* sums = a.sums + (((int64_t)share.z * a.G + id) * a.tiles + tile) * 64 * RP;
     for (int i = threadIdx.x; i < 64 * RP; i += THREADS) {
         int col, j;
         tile_element(i, RP, is_b, col, j);
@@ -898,11 +899,19 @@ __global__ void __launch_bounds__(THREADS, 2) adapter_grad_kernel(const GradArgs
 #pragma unroll 1
     for (int i = threadIdx.x; i < 64 * RP; i += 4 * THREADS) {
         float v[4] = {};
-#pragma unroll 4
-        for (int z = 0; z < splits; ++z)
+        for (int z = 0; z < splits; z += 4) {              // (sixteen loads at a time, the last ones too)
+            float w[4][4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                v[k] += sums[z * next + i + k * THREADS];
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    w[e][k] = z + e < splits ? sums[(z + e) * next + i + k * THREADS] : 0.f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    v[k] += w[e][k];
+        }
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             int col, j;
@@ -1032,7 +1041,7 @@ cudaError_t launch_grad_as(const GradArgs& a, cudaStream_t st)
     using Ring = GradRing<XT, JT>;
     const size_t smem = std::max<size_t>((size_t)(WARPS / (RP / JT)) * 64 * (RP + 2) * 4, (size_t)WARPS * Ring::STAGES * Ring::STAGE);
     static std::atomic<uint64_t> known{0};
-    return launch_cluster<GradArgs>(adapter_grad_kernel<XT, RP, JT>, known, (int)smem, dim3(a.tiles, a.G, a.splits), 1, smem, st, a);
+    return launch_cluster<GradArgs>(adapter_grad_kernel<XT, RP, JT>, known, (int)smem, grad_grid(a), 1, smem, st, a);
 }
 
 template <typename XT>

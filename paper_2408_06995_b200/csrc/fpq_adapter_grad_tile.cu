@@ -6,9 +6,10 @@
 // rows of x lie as they are the MMA's first operand (128 x 64, its 128 columns side by side); the warps write t or u as three BF16
 // terms, which hold all of its 24 bits, side by side as 3 x rank columns of the second operand: one MMA for the three, whose
 // accumulators are added up in registers every 128 rows, the smallest term first (the tensor core cuts its sums off).
-// The last of the blocks that share a sum adds it up in a fixed order.
+// Blocks that share a sum write theirs, and a second kernel adds them up in order.
 //
-// Bound by memory: FIGURES
+// Bound by memory: 30011 x 1280 and x 640, rank 32, three adapters: 25 us, of which 23 read 115 MB in the 285 blocks' main loops, two blocks
+// on an SM; their sums 5 us more (under a profiler, from cold caches).  By warps (fpq_adapter.cu), which split t anew for every 64 columns: 57.
 #include <algorithm>
 #include <atomic>
 
@@ -47,10 +48,10 @@ __global__ void __launch_bounds__(THREADS, GradTile<RP>::ON_AN_SM) adapter_grad_
     const uint32_t bars = base_addr + STAGES * T::STAGE, full = bars, ready = bars + 32, empty = bars + 64, sum_full = bars + 96, sum_free = bars + 112;
     volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(smem + STAGES * T::STAGE + 128);
     volatile int* rows_of = reinterpret_cast<volatile int*>(smem + STAGES * T::STAGE + 144);      // [STAGES]: of the run that lies there; -1: no more
-    volatile int* last = reinterpret_cast<volatile int*>(smem + STAGES * T::STAGE + 176);
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int tile = blockIdx.x, id = blockIdx.y, splits = splits_of(a, id), z = blockIdx.z;
-    if (z >= splits)
+    const GradShare share = share_of(a);
+    const int tile = blockIdx.x, id = share.id, z = share.z, splits = share.splits;
+    if (z < 0)
         return;
     const bool is_b = tile >= a.tiles_k;
     const int64_t D = is_b ? a.N : a.K, c0 = (int64_t)(is_b ? tile - a.tiles_k : tile) * COLS;
@@ -265,51 +266,19 @@ __global__ void __launch_bounds__(THREADS, GradTile<RP>::ON_AN_SM) adapter_grad_
             flag_status(ga.status, FPQ_ERR_TIMEOUT);
     }
 
-    // a thread's sums: of dA one column and SHARE ranks, columns side by side; of dB the ranks side by side
-    const int64_t every = (int64_t)a.G * a.tiles * (COLS * RP);
-    float* sums = a.sums + ((int64_t)id * a.tiles + tile) * (COLS * RP) + (is_b ? col * RP + j0 : j0 * COLS + col);
-    if (splits > 1) {
-        if (warp >= 2) {
-            float* mine = sums + z * every;
-            if (is_b) {
+    // of dA columns lie side by side, of dB ranks
+    if (warp >= 2 && splits > 1) {
+        float* sums = a.sums + (((int64_t)z * a.G + id) * a.tiles + tile) * (COLS * RP) + (is_b ? col * RP + j0 : j0 * COLS + col);
+        if (is_b) {
 #pragma unroll
-                for (int i = 0; i < SHARE; i += 4)
-                    *reinterpret_cast<float4*>(mine + i) = make_float4(sum[i], sum[i + 1], sum[i + 2], sum[i + 3]);
-            } else {
-#pragma unroll
-                for (int i = 0; i < SHARE; ++i)
-                    mine[i * COLS] = sum[i];
-            }
-        }
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            uint32_t ended;
-            asm volatile("atom.acq_rel.gpu.global.add.u32 %0, [%1], 1;" : "=r"(ended) : "l"(a.tickets + (int64_t)id * a.tiles + tile) : "memory");
-            *last = ended == (uint32_t)splits - 1;
-        }
-        __syncthreads();
-        if (*last && warp >= 2) {
+            for (int i = 0; i < SHARE; i += 4)
+                *reinterpret_cast<float4*>(sums + i) = make_float4(sum[i], sum[i + 1], sum[i + 2], sum[i + 3]);
+        } else {
 #pragma unroll
             for (int i = 0; i < SHARE; ++i)
-                sum[i] = 0.f;
-            if (is_b) {
-#pragma unroll 2
-                for (int b = 0; b < splits; ++b)
-#pragma unroll
-                    for (int i = 0; i < SHARE; i += 4) {
-                        const float4 v = *reinterpret_cast<const float4*>(sums + b * every + i);
-                        sum[i] += v.x; sum[i + 1] += v.y; sum[i + 2] += v.z; sum[i + 3] += v.w;
-                    }
-            } else {
-#pragma unroll 2
-                for (int b = 0; b < splits; ++b)
-#pragma unroll
-                    for (int i = 0; i < SHARE; ++i)
-                        sum[i] += sums[b * every + i * COLS];
-            }
+                sums[i * COLS] = sum[i];
         }
-    }
-    if (warp >= 2 && c0 + col < D && (splits == 1 || *last)) {
+    } else if (warp >= 2 && c0 + col < D) {
 #pragma unroll
         for (int i = 0; i < SHARE; ++i)
             if (j0 + i < R)
@@ -321,6 +290,34 @@ __global__ void __launch_bounds__(THREADS, GradTile<RP>::ON_AN_SM) adapter_grad_
         tc_fence_after();
         tmem_dealloc(tmem, T::TMEM);
     }
+}
+
+// The sums of the blocks that share an adapter's rows, in order.  (By the last of those blocks, 19 of them: 13 to 20 us more.)
+template <int RP>
+__global__ void __launch_bounds__(256) adapter_grad_tile_sum_kernel(const GradArgs a)
+{
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    constexpr int PER = COLS * RP / 256;
+    const int tile = blockIdx.x / PER, id = blockIdx.y, i = blockIdx.x % PER * 256 + threadIdx.x, splits = splits_of(a, id);
+    const bool is_b = tile >= a.tiles_k;
+    const int col = is_b ? i / RP : i % COLS, j = is_b ? i % RP : i / COLS;
+    const int64_t c = (int64_t)(is_b ? tile - a.tiles_k : tile) * COLS + col;
+    if (splits == 1 || c >= (is_b ? a.N : a.K) || j >= a.R)
+        return;                                            // (with one, the block itself has stored them)
+    const float* s = a.sums + ((int64_t)id * a.tiles + tile) * (COLS * RP) + i;
+    const int64_t every = (int64_t)a.G * a.tiles * (COLS * RP);
+    float v = 0.f;
+    for (int b = 0; b < splits; b += 8) {                  // (eight loads at a time, the last ones too)
+        float w[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            w[k] = b + k < splits ? s[(b + k) * every] : 0.f;
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            v += w[k];
+    }
+    store_gradient<__nv_bfloat16>(a, id, is_b, c, j, v);
 }
 
 int tiles_of(int64_t n) { return (int)((n + COLS - 1) / COLS); }
@@ -354,7 +351,7 @@ cudaError_t launch_as(const GradArgs& a, cudaStream_t st)
         !encode_rows(enc, &tt, a.t, a.M, a.R, a.R, FPQ_FP32, RUN, RP, false) || !encode_rows(enc, &tu, a.u, a.M, a.R, a.R, FPQ_FP32, RUN, RP, false))
         return cudaErrorUnknown;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(a.tiles, a.G, a.splits);
+    cfg.gridDim = grad_grid(a);
     cfg.blockDim = dim3(THREADS);
     cfg.dynamicSmemBytes = T::SMEM;
     cfg.stream = st;
@@ -363,23 +360,30 @@ cudaError_t launch_as(const GradArgs& a, cudaStream_t st)
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, adapter_grad_tile_kernel<RP>, tx, ty, tt, tu, g);
+    e = cudaLaunchKernelEx(&cfg, adapter_grad_tile_kernel<RP>, tx, ty, tt, tu, g);
+    if (e != cudaSuccess || a.splits == 1)
+        return e;
+    return launch_overlapped(adapter_grad_tile_sum_kernel<RP>, dim3(a.tiles * (COLS * RP / 256), a.G), 256, 0, st, a);
 }
 
 }  // namespace
 
+// From 1024 rows on (whole backward passes, the gradients by warps and so: 1024 rows, 320 -> 320, rank 32: 21.8 and 16.3 us; 65536 rows, 640 ->
+// 2560, rank 64: 505 and 271; 512 rows of 32 adapters, rank 16: 22.4 and 27.2).  Rows that start between 16-byte boundaries, and ranks that are no
+// multiple of four, go by warps.
 bool adapter_grad_tiles_preferred(const GradArgs& a)
 {
     if (a.R > 64 || a.R % 4 != 0 || !mapped(a.x, a.ldx, 2) || !mapped(a.dy, a.ld_dy, 2) || !mapped(a.t, a.R, 4) || !mapped(a.u, a.R, 4))
         return false;
-    return a.M >= 2048;
+    return a.M >= 1024;
 }
 
 // One wave of blocks, 256 rows at least to each.  Of several adapters each gets its share of the rows' blocks (splits_of), rounded up.
 int adapter_grad_tile_splits(int64_t M, int64_t N, int64_t K, int G, int R)
 {
-    const int64_t tiles = tiles_of(K) + tiles_of(N), slots = (R <= 32 ? 2 : 1) * 148, rounded_up = std::min(G - 1, 8) / 2;
-    return (int)std::max<int64_t>(std::min(M / 256, std::min(slots / tiles - rounded_up, 8 * 148 / (tiles * G))), 1);
+    const int64_t tiles = tiles_of(K) + tiles_of(N), fit = (R <= 32 ? 2 : 1) * 148 / tiles;
+    const int64_t most = std::max<int64_t>(fit - (G - 1), fit / 2);
+    return (int)std::max<int64_t>(std::min(M / 256, std::min(most, 8 * 148 / (tiles * G))), 1);
 }
 
 size_t adapter_grad_tile_columns(int64_t M, int64_t N, int64_t K, int G, int R)

@@ -534,6 +534,9 @@ GRAD_TILES = [  # M, K, N, R, cuts, ids, G: BF16 rows whose gradients come from 
     (5000, 136, 520, 64, [0, 2500, 4990], [1, 0], 2),
     (2050, 1288, 72, 40, [0, 1025, 2050], [-1, 0], 1),
     (30000, 64, 64, 8, [0, 29000, 30000], [0, 1], 2),
+    (6000, 128, 64, 8, [0] + list(range(40, 4041, 50)) + [6000], [i % 41 for i in range(81)] + [7], 41),
+    (9000, 64, 128, 24, [0, 8800] + list(range(8801, 8900)), [i % 32 for i in range(100)], 32),
+    (1030, 72, 72, 4, [0, 300, 1029], [1, 0], 2),
 ]
 
 
@@ -554,6 +557,17 @@ def test_gradients_by_tiles(shape):
     check_backward(t, u, *got, torch.zeros_like(dx), base=False)
     again = fpq.fpq_adapter_backward(t["dy"], t["x"], u, t["a"], t["b"], t["offsets"], t["ids"], t["scale"], need_dx=False)
     assert torch.equal(got[1], again[1]) and torch.equal(got[2], again[2])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("xt", [F32, HF])
+@pytest.mark.parametrize("G", [32, 33])
+def test_gradients_of_many_adapters_that_share_blocks(G, xt):
+    cuts = [0, 5000] + [5000 + 13 * i for i in range(1, 60)] + [6400]
+    t = make(6400, 64, 48, 8, cuts, [i * 7 % (G + 1) for i in range(61)], G, xt, xt)
+    u, dx = torch.randn(6400, 8, device="cuda"), torch.zeros_like(t["x"])
+    got = fpq.fpq_adapter_backward(t["dy"], t["x"], u, t["a"], t["b"], t["offsets"], t["ids"], t["scale"], None, dx)
+    check_backward(t, u, *got, torch.zeros_like(dx), base=False)
 
 
 @pytest.mark.gpu
