@@ -48,6 +48,10 @@ __global__ void __launch_bounds__(THREADS, GradTile<RP>::ON_AN_SM) adapter_grad_
     const uint32_t bars = base_addr + STAGES * T::STAGE, full = bars, ready = bars + 32, empty = bars + 64, sum_full = bars + 96, sum_free = bars + 112;
     volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(smem + STAGES * T::STAGE + 128);
     volatile int* rows_of = reinterpret_cast<volatile int*>(smem + STAGES * T::STAGE + 144);      // [STAGES]: of the run that lies there; -1: no more
+    if (threadIdx.x == 0) {
+        tma_prefetch_desc((int)blockIdx.x >= ga.a.tiles_k ? &tm_dy : &tm_x);
+        tma_prefetch_desc((int)blockIdx.x >= ga.a.tiles_k ? &tm_u : &tm_t);
+    }
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const GradShare share = share_of(a);
     const int tile = blockIdx.x, id = share.id, z = share.z, splits = share.splits;
@@ -68,8 +72,6 @@ __global__ void __launch_bounds__(THREADS, GradTile<RP>::ON_AN_SM) adapter_grad_
             mbar_init(sum_free + 8 * b, WORK_WARPS);
         }
         fence_barrier_init();
-        tma_prefetch_desc(is_b ? &tm_dy : &tm_x);
-        tma_prefetch_desc(is_b ? &tm_u : &tm_t);
     }
     if (warp == 1) {
         tmem_alloc(smem_u32((const void*)tmem_slot), T::TMEM);

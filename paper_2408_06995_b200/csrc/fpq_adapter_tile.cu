@@ -11,7 +11,7 @@
 //      them (the rows of a request's last tile, which are fewer, are stored by the warp).
 // Bound by memory: 18944 x 64 -> 2560, BF16, rank 64, one block for every SM: 44 us, 4.4 TB/s; the pass by warps (fpq_adapter.cu), which
 // spends some 300 instructions on 16 x 32 values, 95 us.  A wave of blocks has some 7 us of its own (finding the tile, the first copies,
-// the step from t to y).  32768 x 320 -> 2560, two blocks on an SM: 78 us against 159.
+// the step from t to y).  32768 x 320 -> 2560, two blocks on an SM: 76 us against 159.
 #include <math.h>
 
 #include <algorithm>
@@ -38,7 +38,7 @@ struct TileLayout {
     // W1's part of a stage: the operand as it lies in memory; FP32 rows: with its tails, or 16-bit weights and what they are in FP32
     static constexpr int W_BYTES = RP * 128, W_RAW = FP32 && !WIDE_W ? RP * 64 : W_BYTES, W_MORE = FP32 ? W_BYTES : 0;
     static constexpr int X_PART = X_BYTES * (FP32 ? 2 : 1), STAGE = X_PART + W_RAW + W_MORE;
-    static constexpr int STAGES = TWO ? 2 : FP32 ? 3 : 4;
+    static constexpr int STAGES = FP32 ? (TWO ? 2 : 3) : TWO ? 3 : 4;
     static constexpr int CHUNK = FP32 ? 2 : 4;                                      // stages whose products the tensor core adds up
     static constexpr int T_ROW = RP * (BF ? 2 : 4), KB = (T_ROW + 127) / 128;       // bytes of a row of t, and blocks of 128
     static constexpr int T_BYTES = KB * TILE_M * 128;                               // one term
@@ -132,6 +132,13 @@ __global__ void __launch_bounds__(TileLayout<XT, WT, RP, TWO>::THREADS, TWO ? 2 
     const uint32_t full = bars, ready = bars + 32, empty = bars + 64, t_full = bars + 96, t_free = bars + 112, t_ready = bars + 128,
                    w_full = bars + 136, w_empty = bars + 168, w_ready = bars + 200, y_full = bars + 232, slot_full = bars + 264;   // slot_full: [warp][SLOTS]
     volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(smem_raw + (bars + 480 - smem_u32(smem_raw)));
+    if (threadIdx.x == 0) {
+        tma_prefetch_desc(&tm_x);
+        tma_prefetch_desc(&tm_w1);
+        tma_prefetch_desc(&tm_w2);
+        tma_prefetch_desc(&tm_base);
+        tma_prefetch_desc(&tm_out);
+    }
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -166,11 +173,6 @@ __global__ void __launch_bounds__(TileLayout<XT, WT, RP, TWO>::THREADS, TWO ? 2 
         for (int s = 0; s < WORK_WARPS * SLOTS; ++s)
             mbar_init(slot_full + 8 * s, 1);
         fence_barrier_init();
-        tma_prefetch_desc(&tm_x);
-        tma_prefetch_desc(&tm_w1);
-        tma_prefetch_desc(&tm_w2);
-        tma_prefetch_desc(&tm_base);
-        tma_prefetch_desc(&tm_out);
     }
     if (warp == 1) {
         tmem_alloc(smem_u32((const void*)tmem_slot), T::TMEM);
@@ -208,9 +210,10 @@ __global__ void __launch_bounds__(TileLayout<XT, WT, RP, TWO>::THREADS, TWO ? 2 
             cluster_sync_all();
         }
         if (copier && active && n_chunks > 0 && !dead) {
-            // W2's sets lie where the stages were: they are free when t is there
+            // W2's sets lie where the stages were: they are free when the last MMA on these has ended
             int j = 0;
-            if (!mbar_wait(t_ready, 0))
+            const int last = (n_stages - 1) / T::CHUNK;
+            if (n_stages > 0 && !mbar_wait(t_full + 8 * (last & 1), (last >> 1) & 1))
                 dead = true;
             for (; j < n_chunks && !dead; ++j) {
                 const uint32_t set = j % SETS, at = base_addr + T::W2_BASE + set * T::W2_SET;
@@ -327,6 +330,7 @@ __global__ void __launch_bounds__(TileLayout<XT, WT, RP, TWO>::THREADS, TWO ? 2 
 #pragma unroll
             for (int i = 0; i < SHARE; ++i)
                 sum[i] = 0.f;
+            const float scale = a.scale ? a.scale[tr.id] : 1.f;
             int drained = 0;
             auto drain = [&](int c) {
                 const uint32_t buf = c & 1;
@@ -388,7 +392,6 @@ __global__ void __launch_bounds__(TileLayout<XT, WT, RP, TWO>::THREADS, TWO ? 2 
                 __syncwarp();
                 cluster_sync_all();                        // (nobody reads these sums any more)
             }
-            const float scale = a.scale ? a.scale[tr.id] : 1.f;
             float zero[4] = {};                            // become NaN if a sum is not finite
 #pragma unroll
             for (int i = 0; i < SHARE; ++i)
@@ -418,26 +421,20 @@ __global__ void __launch_bounds__(TileLayout<XT, WT, RP, TWO>::THREADS, TWO ? 2 
             for (int i = 0; i < SHARE; ++i)
                 if (group * SHARE + i >= R || row >= tr.rows)
                     sum[i] = 0.f;
-            if (a.kept && rank == 0 && row < tr.rows) {
-                float* k = a.kept + (tr.row + row) * R + group * SHARE;
-#pragma unroll
-                for (int i = 0; i < SHARE; ++i)
-                    if (group * SHARE + i < R)
-                        k[i] = a.kept_scaled ? sum[i] * scale : sum[i];
-            }
+            float st[SHARE];
 #pragma unroll
             for (int i = 0; i < SHARE; ++i)
-                sum[i] *= scale;
+                st[i] = sum[i] * scale;
 #pragma unroll
             for (int i = 0; i < SHARE; i += 4)
-                *reinterpret_cast<float4*>(mine + i) = make_float4(sum[i], sum[i + 1], sum[i + 2], sum[i + 3]);
+                *reinterpret_cast<float4*>(mine + i) = make_float4(st[i], st[i + 1], st[i + 2], st[i + 3]);
             if (T::BF) {
 #pragma unroll
                 for (int i = 0; i < SHARE; i += 4) {
                     uint32_t h[2], l[2];
 #pragma unroll
                     for (int e = 0; e < 2; ++e)
-                        split_bf16(sum[i + 2 * e], sum[i + 2 * e + 1], h[e], l[e]);
+                        split_bf16(st[i + 2 * e], st[i + 2 * e + 1], h[e], l[e]);
                     const int j = group * SHARE + i, at = swizzled(row, j / 8) + j % 8 * 2;
                     *reinterpret_cast<uint2*>(smem + at) = make_uint2(h[0], h[1]);
                     *reinterpret_cast<uint2*>(smem + T::T_BYTES + at) = make_uint2(l[0], l[1]);
@@ -446,14 +443,29 @@ __global__ void __launch_bounds__(TileLayout<XT, WT, RP, TWO>::THREADS, TWO ? 2 
 #pragma unroll
                 for (int i = 0; i < SHARE; i += 4) {
                     const int j = group * SHARE + i, at = j / 32 * (TILE_M * 128) + swizzled(row, j % 32 / 4);
-                    *reinterpret_cast<float4*>(smem + at) = make_float4(sum[i], sum[i + 1], sum[i + 2], sum[i + 3]);
-                    *reinterpret_cast<float4*>(smem + T::T_BYTES + at) = make_float4(tail(sum[i]), tail(sum[i + 1]), tail(sum[i + 2]), tail(sum[i + 3]));
+                    *reinterpret_cast<float4*>(smem + at) = make_float4(st[i], st[i + 1], st[i + 2], st[i + 3]);
+                    *reinterpret_cast<float4*>(smem + T::T_BYTES + at) = make_float4(tail(st[i]), tail(st[i + 1]), tail(st[i + 2]), tail(st[i + 3]));
                 }
             }
             fence_proxy_async();
             asm volatile("bar.sync 1, %0;" ::"n"(32 * WORK_WARPS) : "memory");                    // all of t is there, for the odd sums too
             if (lane == 0)
                 mbar_arrive(t_ready);
+            if (a.kept && rank == 0 && row < tr.rows) {    // (while the MMAs begin)
+                float* k = a.kept + (tr.row + row) * R + group * SHARE;
+                if (R % 4 == 0 && (reinterpret_cast<uintptr_t>(a.kept) & 15) == 0) {
+#pragma unroll
+                    for (int i = 0; i < SHARE; i += 4)
+                        if (group * SHARE + i < R)
+                            *reinterpret_cast<float4*>(k + i) = a.kept_scaled ? make_float4(st[i], st[i + 1], st[i + 2], st[i + 3])
+                                                                              : make_float4(sum[i], sum[i + 1], sum[i + 2], sum[i + 3]);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < SHARE; ++i)
+                        if (group * SHARE + i < R)
+                            k[i] = a.kept_scaled ? st[i] : sum[i];
+                }
+            }
         } else if (a.kept && rank == 0) {
             for (int i = tid; i < tr.rows * R; i += 32 * WORK_WARPS)
                 a.kept[tr.row * R + i] = 0.f;
