@@ -560,6 +560,16 @@ def test_gradients_by_tiles(shape):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("K,N,ldx,ldy", [(1, 3, 8, 8), (5, 130, 16, 136), (200, 64, 1000, 2000)])
+def test_gradients_by_tiles_in_slices(K, N, ldx, ldy):
+    M, R = 1700, 8
+    t = make(M, K, N, R, [0, 900, 1690], [1, 0], 2, BF, BF, ldx=ldx, ldy=ldy)
+    u, dx = torch.randn(M, R, device="cuda"), torch.zeros(M, K, dtype=BF, device="cuda")
+    got = fpq.fpq_adapter_backward(t["dy"], t["x"], u, t["a"], t["b"], t["offsets"], t["ids"], t["scale"], None, dx)
+    check_backward(t, u, *got, torch.zeros_like(dx), base=False)
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("xt", [F32, HF])
 @pytest.mark.parametrize("G", [32, 33])
 def test_gradients_of_many_adapters_that_share_blocks(G, xt):
