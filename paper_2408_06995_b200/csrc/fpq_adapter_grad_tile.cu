@@ -6,7 +6,7 @@
 // rows of x lie as they are the MMA's first operand (128 x 64, its 128 columns side by side); the warps write t or u as three BF16
 // terms, which hold all of its 24 bits, side by side as 3 x rank columns of the second operand: one MMA for the three, whose
 // accumulators are added up in registers every 128 rows, the smallest term first (the tensor core cuts its sums off).
-// Blocks that share a sum write theirs, and a second kernel adds them up in order.
+// Blocks that share a sum write theirs, and a second kernel adds them up in order.  Ranks above 64 go to two blocks, 64 to each.
 //
 // Bound by memory: 30011 x 1280 and x 640, rank 32, three adapters: 25 us, of which 23 read 115 MB in the 285 blocks' main loops, two blocks
 // on an SM; their sums 5 us more (under a profiler, from cold caches).  By warps (fpq_adapter.cu), which split t anew for every 64 columns: 57.
@@ -49,12 +49,12 @@ __global__ void __launch_bounds__(THREADS, GradTile<RP>::ON_AN_SM) adapter_grad_
     volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(smem + STAGES * T::STAGE + 128);
     volatile int* rows_of = reinterpret_cast<volatile int*>(smem + STAGES * T::STAGE + 144);      // [STAGES]: of the run that lies there; -1: no more
     if (threadIdx.x == 0) {
-        tma_prefetch_desc((int)blockIdx.x >= ga.a.tiles_k ? &tm_dy : &tm_x);
-        tma_prefetch_desc((int)blockIdx.x >= ga.a.tiles_k ? &tm_u : &tm_t);
+        tma_prefetch_desc((int)blockIdx.x % ga.a.tiles >= ga.a.tiles_k ? &tm_dy : &tm_x);
+        tma_prefetch_desc((int)blockIdx.x % ga.a.tiles >= ga.a.tiles_k ? &tm_u : &tm_t);
     }
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const GradShare share = share_of(a);
-    const int tile = blockIdx.x, id = share.id, z = share.z, splits = share.splits;
+    const int part = blockIdx.x / a.tiles, parts = gridDim.x / a.tiles, tile = blockIdx.x % a.tiles, id = share.id, z = share.z, splits = share.splits;
     if (z < 0)
         return;
     const bool is_b = tile >= a.tiles_k;
@@ -138,7 +138,7 @@ __global__ void __launch_bounds__(THREADS, GradTile<RP>::ON_AN_SM) adapter_grad_
                     mbar_expect_tx(full + 8 * s, T::X_BYTES + T::T_BYTES);
                     tma_load_2d(st, is_b ? &tm_dy : &tm_x, full + 8 * s, (int)c0, row);
                     tma_load_2d(st + T::X_BYTES / 2, is_b ? &tm_dy : &tm_x, full + 8 * s, (int)c0 + COLS / 2, row);
-                    tma_load_2d(st + T::X_BYTES + T::B_BYTES, is_b ? &tm_u : &tm_t, full + 8 * s, 0, row);
+                    tma_load_2d(st + T::X_BYTES + T::B_BYTES, is_b ? &tm_u : &tm_t, full + 8 * s, part * RP, row);
                 } else {
                     mbar_arrive(full + 8 * s);
                 }
@@ -270,7 +270,7 @@ __global__ void __launch_bounds__(THREADS, GradTile<RP>::ON_AN_SM) adapter_grad_
 
     // of dA columns lie side by side, of dB ranks
     if (warp >= 2 && splits > 1) {
-        float* sums = a.sums + (((int64_t)z * a.G + id) * a.tiles + tile) * (COLS * RP) + (is_b ? col * RP + j0 : j0 * COLS + col);
+        float* sums = a.sums + ((((int64_t)z * a.G + id) * parts + part) * a.tiles + tile) * (COLS * RP) + (is_b ? col * RP + j0 : j0 * COLS + col);
         if (is_b) {
 #pragma unroll
             for (int i = 0; i < SHARE; i += 4)
@@ -283,8 +283,8 @@ __global__ void __launch_bounds__(THREADS, GradTile<RP>::ON_AN_SM) adapter_grad_
     } else if (warp >= 2 && c0 + col < D) {
 #pragma unroll
         for (int i = 0; i < SHARE; ++i)
-            if (j0 + i < R)
-                store_gradient<__nv_bfloat16>(a, id, is_b, c0 + col, j0 + i, sum[i]);
+            if (part * RP + j0 + i < R)
+                store_gradient<__nv_bfloat16>(a, id, is_b, c0 + col, part * RP + j0 + i, sum[i]);
     }
     tc_fence_before();
     __syncthreads();
@@ -301,14 +301,15 @@ __global__ void __launch_bounds__(256) adapter_grad_tile_sum_kernel(const GradAr
     asm volatile("griddepcontrol.wait;" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     constexpr int PER = COLS * RP / 256;
-    const int tile = blockIdx.x / PER, id = blockIdx.y, i = blockIdx.x % PER * 256 + threadIdx.x, splits = splits_of(a, id);
+    const int part = blockIdx.x / PER / a.tiles, parts = gridDim.x / PER / a.tiles, tile = blockIdx.x / PER % a.tiles, id = blockIdx.y;
+    const int i = blockIdx.x % PER * 256 + threadIdx.x, splits = splits_of(a, id);
     const bool is_b = tile >= a.tiles_k;
-    const int col = is_b ? i / RP : i % COLS, j = is_b ? i % RP : i / COLS;
+    const int col = is_b ? i / RP : i % COLS, j = part * RP + (is_b ? i % RP : i / COLS);
     const int64_t c = (int64_t)(is_b ? tile - a.tiles_k : tile) * COLS + col;
     if (splits == 1 || c >= (is_b ? a.N : a.K) || j >= a.R)
         return;                                            // (with one, the block itself has stored them)
-    const float* s = a.sums + ((int64_t)id * a.tiles + tile) * (COLS * RP) + i;
-    const int64_t every = (int64_t)a.G * a.tiles * (COLS * RP);
+    const float* s = a.sums + (((int64_t)id * parts + part) * a.tiles + tile) * (COLS * RP) + i;
+    const int64_t every = (int64_t)a.G * parts * a.tiles * (COLS * RP);
     float v = 0.f;
     for (int b = 0; b < splits; b += 8) {                  // (eight loads at a time, the last ones too)
         float w[8];
@@ -324,6 +325,7 @@ __global__ void __launch_bounds__(256) adapter_grad_tile_sum_kernel(const GradAr
 
 int tiles_of(int64_t n) { return (int)((n + COLS - 1) / COLS); }
 int padded(int R) { return R <= 16 ? 16 : R <= 32 ? 32 : 64; }
+int parts_of(int R) { return R <= 64 ? 1 : 2; }            // of 64 ranks, which different blocks take
 
 template <int RP>
 cudaError_t launch_as(const GradArgs& a, cudaStream_t st)
@@ -354,6 +356,7 @@ cudaError_t launch_as(const GradArgs& a, cudaStream_t st)
         return cudaErrorUnknown;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grad_grid(a);
+    cfg.gridDim.x *= parts_of(a.R);
     cfg.blockDim = dim3(THREADS);
     cfg.dynamicSmemBytes = T::SMEM;
     cfg.stream = st;
@@ -365,7 +368,7 @@ cudaError_t launch_as(const GradArgs& a, cudaStream_t st)
     e = cudaLaunchKernelEx(&cfg, adapter_grad_tile_kernel<RP>, tx, ty, tt, tu, g);
     if (e != cudaSuccess || a.splits == 1)
         return e;
-    return launch_overlapped(adapter_grad_tile_sum_kernel<RP>, dim3(a.tiles * (COLS * RP / 256), a.G), 256, 0, st, a);
+    return launch_overlapped(adapter_grad_tile_sum_kernel<RP>, dim3(parts_of(a.R) * a.tiles * (COLS * RP / 256), a.G), 256, 0, st, a);
 }
 
 }  // namespace
@@ -375,7 +378,7 @@ cudaError_t launch_as(const GradArgs& a, cudaStream_t st)
 // multiple of four, go by warps.
 bool adapter_grad_tiles_preferred(const GradArgs& a)
 {
-    if (a.R > 64 || a.R % 4 != 0 || !mapped(a.x, a.ldx, 2) || !mapped(a.dy, a.ld_dy, 2) || !mapped(a.t, a.R, 4) || !mapped(a.u, a.R, 4))
+    if (a.R % 4 != 0 || !mapped(a.x, a.ldx, 2) || !mapped(a.dy, a.ld_dy, 2) || !mapped(a.t, a.R, 4) || !mapped(a.u, a.R, 4))
         return false;
     return a.M >= 1024;
 }
@@ -383,14 +386,14 @@ bool adapter_grad_tiles_preferred(const GradArgs& a)
 // One wave of blocks, 256 rows at least to each.  Of several adapters each gets its share of the rows' blocks (splits_of), rounded up.
 int adapter_grad_tile_splits(int64_t M, int64_t N, int64_t K, int G, int R)
 {
-    const int64_t tiles = tiles_of(K) + tiles_of(N), fit = (R <= 32 ? 2 : 1) * 148 / tiles;
+    const int64_t tiles = parts_of(R) * (tiles_of(K) + tiles_of(N)), fit = (R <= 32 ? 2 : 1) * 148 / tiles;
     const int64_t most = std::max<int64_t>(fit - (G - 1), fit / 2);
     return (int)std::max<int64_t>(std::min(M / 256, std::min(most, 8 * 148 / (tiles * G))), 1);
 }
 
 size_t adapter_grad_tile_columns(int64_t M, int64_t N, int64_t K, int G, int R)
 {
-    const size_t splits = R > 64 ? 1 : adapter_grad_tile_splits(M, N, K, G, R);
+    const size_t splits = adapter_grad_tile_splits(M, N, K, G, R);
     return splits == 1 ? 0 : splits * G * (tiles_of(K) + tiles_of(N)) * COLS;
 }
 

@@ -537,6 +537,8 @@ GRAD_TILES = [  # M, K, N, R, cuts, ids, G: BF16 rows whose gradients come from 
     (6000, 128, 64, 8, [0] + list(range(40, 4041, 50)) + [6000], [i % 41 for i in range(81)] + [7], 41),
     (9000, 64, 128, 24, [0, 8800] + list(range(8801, 8900)), [i % 32 for i in range(100)], 32),
     (1030, 72, 72, 4, [0, 300, 1029], [1, 0], 2),
+    (1500, 136, 200, 128, [0, 600, 1499], [1, 0], 2),
+    (5000, 320, 72, 100, [0, 4000, 4500, 5000], [0, 0, 1], 3),
 ]
 
 
