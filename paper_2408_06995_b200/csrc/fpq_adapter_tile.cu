@@ -19,40 +19,14 @@
 #include <type_traits>
 
 #include "fpq_adapter.cuh"
+#include "fpq_adapter_layout.h"
 
 namespace fpq {
 
 namespace {
 
-constexpr int TILE_M = 128, NCOLS = 64;
-constexpr int X_BYTES = TILE_M * 128, SLOT_BYTES = 32 * 128;
-
-// TWO: two blocks on an SM, of eight working warps each; otherwise one of sixteen (of eight, where t takes 64 KB)
 template <typename XT, typename WT, int RP, bool TWO>
-struct TileLayout {
-    static constexpr bool FP32 = sizeof(XT) == 4;
-    static constexpr bool WIDE_W = sizeof(WT) == 4;
-    static constexpr bool BF = std::is_same<XT, __nv_bfloat16>::value;              // t in two BF16 terms, otherwise TF32 terms
-    static constexpr int GROUPS = TWO || (RP == 64 && !BF) ? 2 : 4, WORK_WARPS = 4 * GROUPS, THREADS = 32 * (2 + WORK_WARPS);
-    static constexpr int KE = 128 / (int)sizeof(XT);                                // columns of a stage
-    // W1's part of a stage: the operand as it lies in memory; FP32 rows: with its tails, or 16-bit weights and what they are in FP32
-    static constexpr int W_BYTES = RP * 128, W_RAW = FP32 && !WIDE_W ? RP * 64 : W_BYTES, W_MORE = FP32 ? W_BYTES : 0;
-    static constexpr int X_PART = X_BYTES * (FP32 ? 2 : 1), STAGE = X_PART + W_RAW + W_MORE;
-    static constexpr int STAGES = FP32 ? (TWO ? 2 : 3) : TWO ? 3 : 4;
-    static constexpr int CHUNK = FP32 ? 2 : 4;                                      // stages whose products the tensor core adds up
-    static constexpr int T_ROW = RP * (BF ? 2 : 4), KB = (T_ROW + 127) / 128;       // bytes of a row of t, and blocks of 128
-    static constexpr int T_BYTES = KB * TILE_M * 128;                               // one term
-    // the same of W2, 64 columns
-    static constexpr int W2_BYTES = KB * NCOLS * 128, W2_RAW = BF || WIDE_W ? W2_BYTES : NCOLS * RP * 2, W2_MORE = BF ? 0 : W2_BYTES;
-    static constexpr int W2_SET = (W2_RAW + W2_MORE + 1023) / 1024 * 1024, W2_SETS = GROUPS;       // (a group's own)
-    static constexpr int T_KEPT = TILE_M * RP * 4;                                  // t in FP32, for the cluster and for odd sums
-    static constexpr int W2_BASE = 2 * T_BYTES, KEPT_BASE = W2_BASE + W2_SETS * W2_SET, PHASE2 = KEPT_BASE + T_KEPT;
-    static constexpr int WORK = STAGES * STAGE > PHASE2 ? STAGES * STAGE : PHASE2;
-    static constexpr int SLOTS = TWO || (FP32 && GROUPS == 4) ? 1 : 2;                 // of each warp: 32 rows x 128 bytes of base and y
-    static constexpr int SLOT_BASE = WORK, END = SLOT_BASE + WORK_WARPS * SLOTS * SLOT_BYTES;
-    static constexpr int SMEM = END + 1024;                                         // to start at a multiple of 1024; the barriers lie in front or behind
-    static constexpr int TMEM = 64 * GROUPS;                                        // 2 x rank columns of t, later 64 of y for each group
-};
+using TileLayout = TileSizes<(int)sizeof(XT), (int)sizeof(WT), std::is_same<XT, __nv_bfloat16>::value, RP, TWO>;
 
 struct TileArgs {
     RowsArgs a;
@@ -128,10 +102,11 @@ __global__ void __launch_bounds__(TileLayout<XT, WT, RP, TWO>::THREADS, TWO ? 2 
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base_addr = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* smem = smem_raw + (base_addr - smem_u32(smem_raw));
-    const uint32_t bars = base_addr - smem_u32(smem_raw) >= 512 ? base_addr - 512 : base_addr + T::END;      // 512 bytes
-    const uint32_t full = bars, ready = bars + 32, empty = bars + 64, t_full = bars + 96, t_free = bars + 112, t_ready = bars + 128,
-                   w_full = bars + 136, w_empty = bars + 168, w_ready = bars + 200, y_full = bars + 232, slot_full = bars + 264;   // slot_full: [warp][SLOTS]
-    volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(smem_raw + (bars + 480 - smem_u32(smem_raw)));
+    const uint32_t bars = base_addr + (uint32_t)T::barriers_at((int)(base_addr - smem_u32(smem_raw)));
+    const uint32_t full = bars + T::FULL, empty = bars + T::EMPTY, ready = bars + T::READY, t_full = bars + T::T_FULL, t_free = bars + T::T_FREE,
+                   t_ready = bars + T::T_READY, w_full = bars + T::W_FULL, w_empty = bars + T::W_EMPTY, w_ready = bars + T::W_READY,
+                   y_full = bars + T::Y_FULL, slot_full = bars + T::SLOT_FULL;
+    volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(smem_raw + (bars + T::TMEM_WORD - smem_u32(smem_raw)));
     if (threadIdx.x == 0) {
         tma_prefetch_desc(&tm_x);
         tma_prefetch_desc(&tm_w1);
@@ -156,16 +131,19 @@ __global__ void __launch_bounds__(TileLayout<XT, WT, RP, TWO>::THREADS, TWO ? 2 
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) {
             mbar_init(full + 8 * s, 1);
-            mbar_init(ready + 8 * s, WORK_WARPS);
             mbar_init(empty + 8 * s, 1);
+            if (T::FP32)
+                mbar_init(ready + 8 * s, WORK_WARPS);
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(t_full + 8 * b, 1);
             mbar_init(t_free + 8 * b, WORK_WARPS);
         }
-        for (int b = 0; b < 4; ++b) {
+        for (int b = 0; b < SETS; ++b) {
             mbar_init(w_full + 8 * b, 1);
             mbar_init(w_empty + 8 * b, 1);
+        }
+        for (int b = 0; b < GROUPS; ++b) {
             mbar_init(w_ready + 8 * b, 4);
             mbar_init(y_full + 8 * b, 1);
         }
