@@ -41,8 +41,8 @@ struct TileSizes {
 
     // The barriers, 8 bytes each, and behind the last of them the word that gets the address of the tensor memory
     static constexpr int FULL = 0, EMPTY = FULL + 8 * STAGES, READY = EMPTY + 8 * STAGES;         // (READY: FP32 rows only)
-    static constexpr int T_FULL = READY + (FP32 ? 8 * STAGES : 0), T_FREE = T_FULL + 16, T_READY = T_FREE + 16;
-    static constexpr int W_FULL = T_READY + 8, W_EMPTY = W_FULL + 8 * W2_SETS, W_READY = W_EMPTY + 8 * W2_SETS, Y_FULL = W_READY + 8 * GROUPS;
+    static constexpr int T_FULL = READY + (FP32 ? 8 * STAGES : 0), T_FREE = T_FULL + 16, T_READY = T_FREE + 16, T_DONE = T_READY + 8;
+    static constexpr int W_FULL = T_DONE + 8, W_EMPTY = W_FULL + 8 * W2_SETS, W_READY = W_EMPTY + 8 * W2_SETS, Y_FULL = W_READY + 8 * GROUPS;
     static constexpr int SLOT_FULL = Y_FULL + 8 * GROUPS, TMEM_WORD = SLOT_FULL + 8 * WORK_WARPS * SLOTS;       // SLOT_FULL: [warp][SLOTS]
     static constexpr int BARRIERS = (TMEM_WORD + 4 + 15) / 16 * 16;
 

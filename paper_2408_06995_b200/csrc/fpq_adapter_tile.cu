@@ -104,7 +104,7 @@ __global__ void __launch_bounds__(TileLayout<XT, WT, RP, TWO>::THREADS, TWO ? 2 
     uint8_t* smem = smem_raw + (base_addr - smem_u32(smem_raw));
     const uint32_t bars = base_addr + (uint32_t)T::barriers_at((int)(base_addr - smem_u32(smem_raw)));
     const uint32_t full = bars + T::FULL, empty = bars + T::EMPTY, ready = bars + T::READY, t_full = bars + T::T_FULL, t_free = bars + T::T_FREE,
-                   t_ready = bars + T::T_READY, w_full = bars + T::W_FULL, w_empty = bars + T::W_EMPTY, w_ready = bars + T::W_READY,
+                   t_ready = bars + T::T_READY, t_done = bars + T::T_DONE, w_full = bars + T::W_FULL, w_empty = bars + T::W_EMPTY, w_ready = bars + T::W_READY,
                    y_full = bars + T::Y_FULL, slot_full = bars + T::SLOT_FULL;
     volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(smem_raw + (bars + T::TMEM_WORD - smem_u32(smem_raw)));
     if (threadIdx.x == 0) {
@@ -148,6 +148,7 @@ __global__ void __launch_bounds__(TileLayout<XT, WT, RP, TWO>::THREADS, TWO ? 2 
             mbar_init(y_full + 8 * b, 1);
         }
         mbar_init(t_ready, WORK_WARPS);
+        mbar_init(t_done, 1);
         for (int s = 0; s < WORK_WARPS * SLOTS; ++s)
             mbar_init(slot_full + 8 * s, 1);
         fence_barrier_init();
@@ -188,10 +189,10 @@ __global__ void __launch_bounds__(TileLayout<XT, WT, RP, TWO>::THREADS, TWO ? 2 
             cluster_sync_all();
         }
         if (copier && active && n_chunks > 0 && !dead) {
-            // W2's sets lie where the stages were: they are free when the last MMA on these has ended
+            // W2's sets lie where the stages were: they are free when the last MMA on these has ended.  (A barrier of its own, with one
+            // phase: of t_full this thread has not seen the phases in between, and a parity alone does not tell them apart.)
             int j = 0;
-            const int last = (n_stages - 1) / T::CHUNK;
-            if (n_stages > 0 && !mbar_wait(t_full + 8 * (last & 1), (last >> 1) & 1))
+            if (n_stages > 0 && !mbar_wait(t_done, 0))
                 dead = true;
             for (; j < n_chunks && !dead; ++j) {
                 const uint32_t set = j % SETS, at = base_addr + T::W2_BASE + set * T::W2_SET;
@@ -244,6 +245,8 @@ __global__ void __launch_bounds__(TileLayout<XT, WT, RP, TWO>::THREADS, TWO ? 2 
                 if (++s == STAGES) { s = 0; ph ^= 1; }
                 if ((k + 1) % CHUNK == 0 || k + 1 == n_stages)
                     mma_commit(t_full + 8 * buf);
+                if (k + 1 == n_stages)
+                    mma_commit(t_done);
             }
         }
         __syncwarp();

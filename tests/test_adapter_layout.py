@@ -10,7 +10,7 @@ from paper_2408_06995_b200 import build as fpq_build
 FORMS = [(4, wb, 0, rp, two) for wb in (4, 2) for rp in (32, 64) for two in (0, 1) if rp == 32 or not two]
 FORMS += [(2, 2, bf, rp, two) for bf in (0, 1) for rp in (16, 32, 64) for two in (0, 1) if rp <= 32 or bf or not two]
 NAMES = ["FP32", "STAGES", "STAGE", "W2_SETS", "GROUPS", "WORK_WARPS", "SLOTS", "SLOT_BASE", "END", "SMEM", "W2_BASE", "W2_SET", "KEPT_BASE", "T_KEPT",
-         "T_BYTES", "FULL", "EMPTY", "READY", "T_FULL", "T_FREE", "T_READY", "W_FULL", "W_EMPTY", "W_READY", "Y_FULL", "SLOT_FULL", "TMEM_WORD",
+         "T_BYTES", "FULL", "EMPTY", "READY", "T_FULL", "T_FREE", "T_READY", "T_DONE", "W_FULL", "W_EMPTY", "W_READY", "Y_FULL", "SLOT_FULL", "TMEM_WORD",
          "BARRIERS"]
 
 
@@ -42,7 +42,7 @@ def apart(ranges):
 @pytest.mark.parametrize("form", FORMS, ids=lambda f: "-".join(map(str, f)))
 def test_barriers_and_the_tensor_memory_word_lie_apart(sizes, form):
     t, places = sizes[form]
-    counts = {"FULL": t["STAGES"], "EMPTY": t["STAGES"], "READY": t["STAGES"] if t["FP32"] else 0, "T_FULL": 2, "T_FREE": 2, "T_READY": 1,
+    counts = {"FULL": t["STAGES"], "EMPTY": t["STAGES"], "READY": t["STAGES"] if t["FP32"] else 0, "T_FULL": 2, "T_FREE": 2, "T_READY": 1, "T_DONE": 1,
               "W_FULL": t["W2_SETS"], "W_EMPTY": t["W2_SETS"], "W_READY": t["GROUPS"], "Y_FULL": t["GROUPS"],
               "SLOT_FULL": t["WORK_WARPS"] * t["SLOTS"]}
     barriers = [(t[n] + 8 * i, t[n] + 8 * i + 8) for n, k in counts.items() for i in range(k)]
