@@ -259,14 +259,15 @@ __global__ void __launch_bounds__(THREADS, RP <= 64 ? 2 : 1) adapter_rows_kernel
                 }
             } else {
                 const int by = is_x ? a.in_by : a.base_by;
+                const XT* anywhere = (const XT*)(is_x ? a.in : a.base);      // (what is not copied has a source too, aligned like the others)
                 if (by == 16) {
 #pragma unroll 1
                     for (int k = 0; k < 16; k += EVERY) {
                         const bool there = cr + k < here && col < width;
-                        copy_async16(smem_u32(dst + k * (32 * (int)sizeof(XT))), there ? src + k * ld : in, there);
+                        copy_async16(smem_u32(dst + k * (32 * (int)sizeof(XT))), there ? src + k * ld : anywhere, there);
                     }
                 } else {
-                    copy_pieces<XT, 16 / EVERY>(dst, EVERY * 32 * (int)sizeof(XT), src, EVERY * ld, here - cr, EVERY, width - col, by, in);
+                    copy_pieces<XT, 16 / EVERY>(dst, EVERY * 32 * (int)sizeof(XT), src, EVERY * ld, here - cr, EVERY, width - col, by, anywhere);
                 }
             }
         }

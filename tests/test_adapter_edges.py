@@ -29,3 +29,15 @@ def test_tiles_of_few_stages(M, R, K, xt, wt):
     for _ in range(3):
         assert torch.equal(A.run_forward(t)[1], first[1])
     assert fpq.fpq_read_status() == fpq.OK
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("xt", [BF, HF, F32])
+@pytest.mark.parametrize("K,N,ldx,ldy", [(257, 96, 257, 96), (96, 257, 96, 257), (96, 130, 98, 131), (131, 96, 131, 98), (64, 64, 67, 72), (64, 64, 72, 67)])
+def test_rows_and_base_of_different_alignment(K, N, ldx, ldy, xt):
+    """Rows of x, or of dy, that start between words while those of base allow wider copies, and the other way round."""
+    t = A.make(210, K, N, 16, [1, 12, 101, 103, 207], [1, 0, 1, 0], 2, xt, xt, ldx=ldx, ldy=ldy)
+    A.check_forward(t, *A.run_forward(t, ldy=ldy))
+    u, dx = torch.randn(210, 16, device="cuda"), torch.full((210, ldx), -7.0, dtype=xt, device="cuda")[:, :K]
+    before = dx.clone()
+    A.check_backward(t, u, *backward(t, u, base=t["dbase"], dx=dx), before)
