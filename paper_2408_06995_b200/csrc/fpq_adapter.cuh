@@ -197,6 +197,16 @@ struct GradArgs {
     int splits;
 };
 
+// whether any row is adapter `id`'s
+__device__ __forceinline__ bool has_rows(const GradArgs& a, int id)
+{
+#pragma unroll 1
+    for (int sg = 0; sg < a.S; ++sg)
+        if (a.ids[sg] == id && min(max(a.offsets[sg + 1], 0), (int)a.M) > min(max(a.offsets[sg], 0), (int)a.M))
+            return true;
+    return false;
+}
+
 template <typename XT>
 __device__ __forceinline__ void store_gradient(const GradArgs& a, int id, bool is_b, int64_t col, int j, float v)
 {
@@ -213,9 +223,12 @@ __device__ __forceinline__ void store_gradient(const GradArgs& a, int id, bool i
                 v = fmaf(as_float(wide[r * ld]), thin[r * a.R], v);
         }
     }
-    if (is_b)
-        a.db[((int64_t)id * a.N + col) * a.R + j] = a.scale ? v * a.scale[id] : v;
-    else
+    if (is_b) {
+        float scaled = a.scale ? v * a.scale[id] : v;
+        if (!finite(scaled) && v == 0.f && !has_rows(a, id))
+            scaled = 0.f;                                  // (nothing was added up; a zero sum of some rows times infinity is NaN)
+        a.db[((int64_t)id * a.N + col) * a.R + j] = scaled;
+    } else
         a.da[((int64_t)id * a.R + j) * a.K + col] = v;
 }
 

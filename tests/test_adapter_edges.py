@@ -41,3 +41,19 @@ def test_rows_and_base_of_different_alignment(K, N, ldx, ldy, xt):
     u, dx = torch.randn(210, 16, device="cuda"), torch.full((210, ldx), -7.0, dtype=xt, device="cuda")[:, :K]
     before = dx.clone()
     A.check_backward(t, u, *backward(t, u, base=t["dbase"], dx=dx), before)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("value", [float("inf"), float("nan")])
+@pytest.mark.parametrize("xt,M", [(F32, 60), (F32, 3000), (BF, 60), (BF, 3000)])
+def test_an_adapter_without_rows_has_zeros_whatever_its_scale(xt, M, value):
+    t = A.make(M, 64, 96, 8, [0, M // 3, M // 3, M], [0, 1, 2], 4, xt, xt)
+    t["scale"][1] = t["scale"][3] = value                  # an empty segment's adapter, and one that no segment names
+    u = torch.randn(M, 8, device="cuda")
+    _, da, db = backward(t, u)
+    for g in (1, 3):
+        assert not bool(da[g].any()) and not bool(db[g].any())
+    t["scale"][2] = value                                  # with rows: zeros of u times it are NaN, as the formula has it
+    u[:, 5] = 0
+    _, da, db = backward(t, u)
+    assert bool(torch.isnan(db[2][:, 5]).all()) and not bool(torch.isfinite(db[2]).any()) and bool(torch.isfinite(db[0]).all())
