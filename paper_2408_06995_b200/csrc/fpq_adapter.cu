@@ -1117,8 +1117,9 @@ cudaError_t launch_adapter_backward(const AdapterProblem& p, const void* dy, int
     uint8_t* bt = at + pad16((size_t)p.G * p.K * padded_ranks(p.R, (int)wb) * wb);
     uint32_t* tickets = (uint32_t*)(bt + pad16((size_t)p.G * p.R * padded_columns(p.N, (int)wb) * wb));
     GradArgs b = {};
-    b.x = x; b.dy = dy; b.t = t; b.u = u; b.scale = p.scale; b.offsets = p.offsets; b.ids = p.ids; b.da = da; b.db = db;
+    b.x = x; b.dy = dy; b.t = t; b.u = u; b.offsets = p.offsets; b.ids = p.ids; b.da = da; b.db = db;
     b.M = p.M; b.N = p.N; b.K = p.K; b.ldx = ldx; b.ld_dy = ld_dy; b.G = p.G; b.R = p.R; b.S = p.M > 0 ? p.S : 0;
+    b.scale = b.S > 0 ? p.scale : nullptr;                 // (without rows the callers have not looked at the scales)
     b.x_by = bytes_at_a_time(x, ldx, p.K, xb);
     b.dy_by = bytes_at_a_time(dy, ld_dy, p.N, xb);
     b.tiles_k = column_tiles(p.K);

@@ -57,3 +57,14 @@ def test_an_adapter_without_rows_has_zeros_whatever_its_scale(xt, M, value):
     u[:, 5] = 0
     _, da, db = backward(t, u)
     assert bool(torch.isnan(db[2][:, 5]).all()) and not bool(torch.isfinite(db[2]).any()) and bool(torch.isfinite(db[0]).all())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("sizes", [{"M": 0}, {"S": 0}])
+def test_without_rows_only_the_gradients_are_touched(sizes):
+    """The other arguments may be anything: a scale between words is no error, and is not read."""
+    da, db, scale = torch.ones(2, 4, 16, device="cuda"), torch.ones(2, 8, 4, device="cuda"), torch.ones(4, device="cuda")
+    call = A.Call(ld_base=16, da=da.data_ptr(), db=db.data_ptr(), scale=scale.data_ptr() + 2, workspace=None, x=None, dy=None, u=None, a=None, b=None,
+                  offsets=None, ids=None, base=None, dx=None, stream=torch.cuda.current_stream().cuda_stream, **sizes)
+    assert call.run("backward") == fpq.OK
+    assert not bool(da.any()) and not bool(db.any())
