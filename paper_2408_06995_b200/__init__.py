@@ -490,10 +490,11 @@ def fpq_adapter_forward(x: torch.Tensor, a: torch.Tensor, b: torch.Tensor, offse
                         y: torch.Tensor = None, u: torch.Tensor = None) -> torch.Tensor:
     """y[i] = base[i] + scale[g] B[g] (A[g] x[i]) for the rows i of segment s, g = ids[s].  x [M][K], base and y [M][N] of float32,
     bfloat16 or float16 (rows may lie apart); a [G][R][K], b [G][N][R]; offsets int32 [S + 1], ids int32 [S].  base may be y; without y a
-    new one is made, in which rows outside of the segments are base's (zeros without a base).  u: None, or [M][R] float32 that
-    receives A[g] x[i], which the backward pass reads."""
+    new one is made, a copy of base first, in which rows outside of the segments stay base's (zeros without a base); it has no autograd
+    history (fpq_adapter_backward gives the gradients).  u: None, or [M][R] float32 that receives A[g] x[i], which the backward
+    pass reads."""
     if y is None:
-        y = base.clone(memory_format=torch.contiguous_format) if base is not None else x.new_zeros((x.shape[0], b.shape[1]))
+        y = base.detach().clone(memory_format=torch.contiguous_format) if base is not None else x.new_zeros((x.shape[0], b.shape[1]))
     code = (_layers or _load_layers()).adapter_forward(x, a, b, offsets, ids, scale, base, y, u)
     if code:
         raise FpqError(code, "fpq_adapter_forward")
@@ -520,7 +521,7 @@ def fpq_adapter_backward(dy: torch.Tensor, x: torch.Tensor, u: torch.Tensor, a: 
     if not need_dx:
         dx = base = None
     elif dx is None:
-        dx = base.clone(memory_format=torch.contiguous_format) if base is not None else torch.zeros_like(x, memory_format=torch.contiguous_format)
+        dx = base.detach().clone(memory_format=torch.contiguous_format) if base is not None else torch.zeros_like(x, memory_format=torch.contiguous_format)
     if da is None:
         da = torch.empty(a.shape, dtype=torch.float32, device=a.device)
     if db is None:

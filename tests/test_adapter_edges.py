@@ -68,3 +68,29 @@ def test_without_rows_only_the_gradients_are_touched(sizes):
                   offsets=None, ids=None, base=None, dx=None, stream=torch.cuda.current_stream().cuda_stream, **sizes)
     assert call.run("backward") == fpq.OK
     assert not bool(da.any()) and not bool(db.any())
+
+
+class Layers:
+    """Stands in for the extension: remembers the call, computes nothing."""
+
+    def adapter_forward(self, *args):
+        self.args = args
+        return 0
+
+    adapter_backward = adapter_forward
+
+
+@pytest.mark.parametrize("with_base", [True, False])
+def test_outputs_made_by_the_call_have_no_history(monkeypatch, with_base):
+    """The kernels' results are no function of `base` alone: an autograd graph that says so would lose every other gradient without a word."""
+    layers = Layers()
+    monkeypatch.setattr(fpq, "_layers", layers)
+    x, a, b = torch.randn(6, 8, requires_grad=True), torch.randn(1, 2, 8, requires_grad=True), torch.randn(1, 4, 2, requires_grad=True)
+    offsets, ids = torch.tensor([0, 6], dtype=torch.int32), torch.zeros(1, dtype=torch.int32)
+    base = torch.randn(6, 4, requires_grad=True) if with_base else None
+    y = fpq.fpq_adapter_forward(x, a, b, offsets, ids, base=base)
+    assert not y.requires_grad and y.grad_fn is None and layers.args[7] is y
+    assert torch.equal(y, base if with_base else torch.zeros(6, 4)) and (not with_base or y.data_ptr() != base.data_ptr())
+    dbase = torch.randn(6, 8, requires_grad=True) if with_base else None
+    for g in fpq.fpq_adapter_backward(torch.randn(6, 4), x, torch.randn(6, 2), a, b, offsets, ids, base=dbase):
+        assert not g.requires_grad and g.grad_fn is None
