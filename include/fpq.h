@@ -480,7 +480,7 @@ fpq_status fpq_adapter_backward(const void* dy, int64_t ld_dy, const void* x, in
  *     p = p (1 - rate weight_decay) - rate / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
  *   tensors_host  HOST array of count descriptors (read during the call): p [n] FP32 updated in place, g [n] of g_type
  *            (FPQ_FP32, FPQ_BF16, FPQ_FP16), m and v [n] updated in place, copy: NULL or [n] of copy_type (FPQ_BF16 or
- *            FPQ_FP16) that receives the new p rounded once.  n = 0 is allowed.  No two buffers may overlap.
+ *            FPQ_FP16) that receives the new p rounded once.  n = 0 is allowed.  What is written overlaps nothing else.
  *   state_type  FPQ_FP32: m and v are FP32, m_scale and v_scale are not used;
  *            FPQ_E4M3_BLOCK32: m and v are E4M3 codes (bias 7) of the first moment and of the SQUARE ROOT of the second,
  *            m_scale and v_scale [ceil(n / 32)] bytes b, each the scale 2^(b - 127) of 32 codes (value = code * scale).

@@ -10,6 +10,7 @@ missing the import of a symbol fails.
 """
 from __future__ import annotations
 
+import bisect
 import ctypes
 import importlib.util
 import os
@@ -558,38 +559,44 @@ class AdamwTable:
         self.device = params[0].get_device() if count else None
         assert self.g_type >= 0, "gradients: expected float32, bfloat16 or float16"
         self._table = (_CAdamwTensor * count)()
-        written = set()
+        written, read = [], []                             # the buffers' bytes: (first, behind the last)
 
-        def pointer(t, n, dtypes, what, optional=False):
+        def pointer(t, n, dtypes, what, optional=False, places=written):
             if t is None and optional:
                 return None
             assert t is not None and t.is_cuda and t.get_device() == self.device and t.dtype in dtypes and t.is_contiguous() and t.numel() == n, \
                 f"{what}: expected a contiguous tensor of {n} elements of {' or '.join(map(str, dtypes))} on the parameters' device"
-            return t.data_ptr()
+            at = t.data_ptr()
+            if n:
+                places.append((at, at + n * t.element_size()))
+            return at
 
         for i, p in enumerate(params):
             n, e = p.numel(), self._table[i]
             blocks = -(-n // 32)
             e.n = n
             e.p = pointer(p, n, (torch.float32,), "params")
-            e.g = pointer(grads[i], n, (grads[0].dtype,), "grads")
+            e.g = pointer(grads[i], n, (grads[0].dtype,), "grads", places=read)
             e.copy = pointer(copies[i], n, (torch.bfloat16, torch.float16), "copies", True)
             if self.state_type == FP32:
                 e.m, e.v = pointer(m[i], n, (torch.float32,), "m"), pointer(v[i], n, (torch.float32,), "v")
             else:
                 e.m, e.v = pointer(m[i], n, codes, "m"), pointer(v[i], n, codes, "v")
                 e.m_scale, e.v_scale = pointer(m_scale[i], blocks, scales, "m_scale"), pointer(v_scale[i], blocks, scales, "v_scale")
-            if n:
-                mine = [q for q in (e.p, e.m, e.v, e.m_scale, e.v_scale, e.copy) if q]
-                assert len(set(mine)) == len(mine) and written.isdisjoint(mine), "a buffer appears twice"
-                written.update(mine)
+        written.sort()
+        assert all(a[1] <= b[0] for a, b in zip(written, written[1:])), "buffers overlap, or one appears twice"
+        starts = [a for a, _ in written]
+        for first, behind in read:                         # (the last written buffer that starts in front of a gradient's end)
+            at = bisect.bisect_left(starts, behind)
+            assert at == 0 or written[at - 1][1] <= first, "gradients overlap what the step writes"
         self._kept = given
 
 
 def fpq_adamw_table(params, grads, m, v, m_scale=None, v_scale=None, copies=None) -> AdamwTable:
     """The list of tensors for fpq_adamw_step.  params: float32; grads: one type of float32, bfloat16, float16; m, v: float32, or E4M3
     codes (uint8 or float8_e4m3fn; v holds the square root of the second moment) with m_scale, v_scale, one byte (uint8 or
-    float8_e8m0fnu) per 32 elements; copies: None, or bfloat16 / float16 tensors (or None for some) that receive the new parameters."""
+    float8_e8m0fnu) per 32 elements; copies: None, or bfloat16 / float16 tensors (or None for some) that receive the new parameters.
+    Buffers that the step writes may overlap neither each other nor a gradient."""
     return AdamwTable(params, grads, m, v, m_scale, v_scale, copies)
 
 
