@@ -568,7 +568,7 @@ class AdamwTable:
                 f"{what}: expected a contiguous tensor of {n} elements of {' or '.join(map(str, dtypes))} on the parameters' device"
             at = t.data_ptr()
             if n:
-                places.append((at, at + n * t.element_size()))
+                places.append((at, at + n * t.dtype.itemsize))
             return at
 
         for i, p in enumerate(params):

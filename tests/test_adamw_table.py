@@ -20,9 +20,6 @@ class Memory:
     def numel(self):
         return self.n
 
-    def element_size(self):
-        return torch.empty(0, dtype=self.dtype).element_size()
-
     def get_device(self):
         return 0
 
@@ -39,7 +36,7 @@ def memory_table(codes=False, **changed):
         given[name] = []
         for n in (64, 40):
             given[name].append(Memory(at, -(-n // unit), dtype))
-            at += given[name][-1].numel() * given[name][-1].element_size()
+            at += given[name][-1].numel() * dtype.itemsize
     for name, (i, place) in changed.items():
         given[name][i] = Memory(place(given), given[name][i].n, given[name][i].dtype)
     if not codes:
