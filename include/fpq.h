@@ -461,11 +461,15 @@ fpq_status fpq_adapter_forward(const void* x, int64_t ldx, int32_t x_type, const
                                void* stream);
 /* Which kernel fpq_adapter_forward runs for contiguous, 16-byte aligned tensors (for logs, benchmarks and tests; nothing is
  * launched): FPQ_ADAPTER_WARPS, by warp-level MMAs on 16 to 128 rows a block; FPQ_ADAPTER_TILES, by tcgen05 MMAs on tiles of
- * 128 rows, for requests of many rows; negative: the error that the call would return.  The first half of the backward pass is
- * the same kernel with N and K exchanged, if dx is wanted. */
+ * 128 rows, for requests of many rows; negative: the error that the call would return.  (Tiles need rows of A and B that are
+ * multiples of 16 bytes: with 16-bit weights a rank that is a multiple of 8.) */
 enum { FPQ_ADAPTER_WARPS = 0, FPQ_ADAPTER_TILES = 1 };
 int32_t fpq_adapter_route(int64_t M, int64_t N, int64_t K, int32_t G, int32_t R, int32_t S, int32_t x_type, int32_t w_type,
                           int32_t has_base);
+/* The same of the first half of fpq_adapter_backward, which forms t and dx from dy (has_dx: with dx; has_base: with base).  Its weights
+ * are transposed and their rows padded to 16 bytes, so any rank up to 64 may take tiles. */
+int32_t fpq_adapter_backward_route(int64_t M, int64_t N, int64_t K, int32_t G, int32_t R, int32_t S, int32_t x_type, int32_t w_type,
+                                   int32_t has_dx, int32_t has_base);
 size_t fpq_adapter_backward_workspace_size(int64_t M, int64_t N, int64_t K, int32_t G, int32_t R, int32_t w_type);
 fpq_status fpq_adapter_backward(const void* dy, int64_t ld_dy, const void* x, int64_t ldx, int32_t x_type, const float* u,
                                 const void* a, const void* b, int32_t w_type, const float* scale, int32_t G, int32_t R,

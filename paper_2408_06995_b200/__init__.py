@@ -83,7 +83,8 @@ EXPORTS = [
     "fpq_zero_census", "fpq_prepared_size_split", "fpq_prepare_weight_split", "fpq_conv2d_split_workspace_size",
     "fpq_conv2d_split", "fpq_set_path_policy", "fpq_get_path_policy", "fpq_read_status", "fpq_status_string",
     "fpq_conv2d_route", "fpq_linear_contraction", "fpq_conv2d_contraction", "fpq_selftest_bounded_wait",
-    "fpq_adapter_forward", "fpq_adapter_route", "fpq_adapter_backward_workspace_size", "fpq_adapter_backward", "fpq_adamw_step",
+    "fpq_adapter_forward", "fpq_adapter_route", "fpq_adapter_backward_route", "fpq_adapter_backward_workspace_size", "fpq_adapter_backward",
+    "fpq_adamw_step",
 ]
 
 _lib = None
@@ -175,6 +176,8 @@ def lib() -> ctypes.CDLL:
         L.fpq_adapter_forward.argtypes = [vp, i64, i32, vp, vp, i32, vp, i32, i32, vp, vp, i32, vp, i64, vp, i64, vp, i64, i64, i64, vp]
         L.fpq_adapter_route.restype = i32
         L.fpq_adapter_route.argtypes = [i64, i64, i64, i32, i32, i32, i32, i32, i32]
+        L.fpq_adapter_backward_route.restype = i32
+        L.fpq_adapter_backward_route.argtypes = [i64, i64, i64, i32, i32, i32, i32, i32, i32, i32]
         L.fpq_adapter_backward_workspace_size.restype = sz
         L.fpq_adapter_backward_workspace_size.argtypes = [i64, i64, i64, i32, i32, i32]
         L.fpq_adapter_backward.restype = i32
@@ -507,6 +510,15 @@ def fpq_adapter_route(M: int, N: int, K: int, G: int, R: int, S: int, x_type: in
     r = lib().fpq_adapter_route(M, N, K, G, R, S, x_type, w_type, int(has_base))
     if r < 0:
         _check(r, "fpq_adapter_route")
+    return r
+
+
+def fpq_adapter_backward_route(M: int, N: int, K: int, G: int, R: int, S: int, x_type: int, w_type: int, need_dx: bool = True,
+                               has_base: bool = True) -> int:
+    """Which kernel the first half of fpq_adapter_backward (t and dx from dy) would run for contiguous tensors of these sizes (ADAPTER_*)."""
+    r = lib().fpq_adapter_backward_route(M, N, K, G, R, S, x_type, w_type, int(need_dx), int(has_base))
+    if r < 0:
+        _check(r, "fpq_adapter_backward_route")
     return r
 
 

@@ -1068,6 +1068,22 @@ cudaError_t launch_transpose_as(const AdapterProblem& p, T* at, T* bt, uint32_t*
 
 size_t pad16(size_t n) { return (n + 15) / 16 * 16; }
 
+// what the rows' pass of a backward call looks like; its weights are the transposed and padded ones
+RowsArgs backward_rows(const AdapterProblem& p, const void* dy, int64_t ld_dy, const void* base, int64_t ld_base, void* dx, int64_t ld_dx, const void* at,
+                       const void* bt)
+{
+    const int wb = type_bytes(p.w_type);
+    RowsArgs a = {};
+    a.in = dy; a.w1 = bt; a.w2 = at; a.scale = p.scale; a.offsets = p.offsets; a.ids = p.ids;
+    a.base = base; a.out = dx; a.kept_scaled = 1;
+    a.ld_w1 = padded_columns(p.N, wb); a.ld_w2 = padded_ranks(p.R, wb);
+    a.M = p.M; a.D1 = p.N; a.D2 = p.K; a.ld_in = ld_dy; a.ld_base = ld_base; a.ld_out = ld_dx;
+    a.G = p.G; a.R = p.R; a.S = p.S;
+    return a;
+}
+
+const void* const ALIGNED = reinterpret_cast<const void*>((uintptr_t)256);     // never followed: only its alignment is looked at
+
 }  // namespace
 
 cudaError_t launch_adapter_forward(const AdapterProblem& p, const void* x, int64_t ldx, const void* base, int64_t ld_base, void* y,
@@ -1084,13 +1100,18 @@ cudaError_t launch_adapter_forward(const AdapterProblem& p, const void* x, int64
 
 bool adapter_forward_by_tiles(const AdapterProblem& p, bool base)
 {
-    const void* there = reinterpret_cast<const void*>((uintptr_t)256);      // never followed: only alignment is looked at
     RowsArgs a = {};
-    a.in = a.w1 = a.w2 = there;
-    a.out = (void*)there;
-    a.base = base ? there : nullptr;
+    a.in = a.w1 = a.w2 = ALIGNED;
+    a.out = (void*)ALIGNED;
+    a.base = base ? ALIGNED : nullptr;
     a.ld_w1 = p.K; a.ld_w2 = p.R;
     a.M = p.M; a.D1 = a.ld_in = p.K; a.D2 = a.ld_out = a.ld_base = p.N; a.G = p.G; a.R = p.R; a.S = p.S;
+    return p.M > 0 && p.S > 0 && adapter_tiles_preferred(a, p.x_type, p.w_type);
+}
+
+bool adapter_backward_by_tiles(const AdapterProblem& p, bool dx, bool base)
+{
+    const RowsArgs a = backward_rows(p, ALIGNED, p.N, dx && base ? ALIGNED : nullptr, p.K, dx ? (void*)ALIGNED : nullptr, p.K, ALIGNED, ALIGNED);
     return p.M > 0 && p.S > 0 && adapter_tiles_preferred(a, p.x_type, p.w_type);
 }
 
@@ -1134,12 +1155,8 @@ cudaError_t launch_adapter_backward(const AdapterProblem& p, const void* dy, int
                                 : launch_transpose_as(p, (uint16_t*)at, (uint16_t*)bt, tickets, n_tickets, st);
         if (e != cudaSuccess)
             return e;
-        RowsArgs a = {};
-        a.in = dy; a.w1 = bt; a.w2 = at; a.scale = p.scale; a.offsets = p.offsets; a.ids = p.ids;
-        a.base = base; a.out = dx; a.kept = t; a.kept_scaled = 1;
-        a.ld_w1 = padded_columns(p.N, (int)wb); a.ld_w2 = padded_ranks(p.R, (int)wb);
-        a.M = p.M; a.D1 = p.N; a.D2 = p.K; a.ld_in = ld_dy; a.ld_base = ld_base; a.ld_out = ld_dx;
-        a.G = p.G; a.R = p.R; a.S = p.S;
+        RowsArgs a = backward_rows(p, dy, ld_dy, base, ld_base, dx, ld_dx, at, bt);
+        a.kept = t;
         e = launch_rows(a, p.x_type, p.w_type, st);
         if (e != cudaSuccess)
             return e;

@@ -1483,6 +1483,14 @@ int32_t fpq_adapter_route(int64_t M, int64_t N, int64_t K, int32_t G, int32_t R,
     return s != FPQ_OK ? s : adapter_forward_by_tiles(p, has_base != 0) ? FPQ_ADAPTER_TILES : FPQ_ADAPTER_WARPS;
 }
 
+int32_t fpq_adapter_backward_route(int64_t M, int64_t N, int64_t K, int32_t G, int32_t R, int32_t S, int32_t x_type, int32_t w_type, int32_t has_dx,
+                                   int32_t has_base)
+{
+    const AdapterProblem p = {nullptr, nullptr, nullptr, nullptr, nullptr, x_type, w_type, G, R, S, M, N, K};
+    const fpq_status s = check_adapters(p);
+    return s != FPQ_OK ? s : adapter_backward_by_tiles(p, has_dx != 0, has_base != 0) ? FPQ_ADAPTER_TILES : FPQ_ADAPTER_WARPS;
+}
+
 size_t fpq_adapter_backward_workspace_size(int64_t M, int64_t N, int64_t K, int32_t G, int32_t R, int32_t w_type)
 {
     const AdapterProblem p = {nullptr, nullptr, nullptr, nullptr, nullptr, FPQ_FP32, w_type, G, R, 0, M, N, K};

@@ -181,6 +181,7 @@ cudaError_t launch_adapter_backward(const AdapterProblem& p, const void* dy, int
                                     const void* base, int64_t ld_base, void* dx, int64_t ld_dx, float* da, float* db, void* workspace,
                                     cudaStream_t st);
 bool adapter_forward_by_tiles(const AdapterProblem& p, bool base);      // which pass runs for contiguous, aligned tensors
+bool adapter_backward_by_tiles(const AdapterProblem& p, bool dx, bool base);
 size_t adapter_backward_bytes(int64_t M, int64_t N, int64_t K, int G, int R, int w_type);
 fpq_status launch_adamw(const fpq_adamw_tensor* t, int count, int g_type, int copy_type, int state_type, const fpq_adamw_options& o,
                         const float* factors, int64_t* step, cudaStream_t st);

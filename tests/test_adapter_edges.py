@@ -94,3 +94,56 @@ def test_outputs_made_by_the_call_have_no_history(monkeypatch, with_base):
     dbase = torch.randn(6, 8, requires_grad=True) if with_base else None
     for g in fpq.fpq_adapter_backward(torch.randn(6, 4), x, torch.randn(6, 2), a, b, offsets, ids, base=dbase):
         assert not g.requires_grad and g.grad_fn is None
+
+
+# tall requests whose backward pass goes by tiles, on padded weights, while the forward pass may not: M, K, N, R, cuts, ids, G
+TALL_ODD_RANKS = [
+    (8192, 1280, 640, 36, [0, 8192], [0], 1),
+    (9000, 640, 1288, 20, [0, 1, 4400, 8999], [1, 0, 1], 2),
+    (18900, 1288, 648, 18, [3, 9000, 18899], [1, 0], 2),
+    (28001, 648, 1288, 12, [0, 14000, 28001], [0, 1], 2),
+    (28000, 1288, 648, 28, [1, 20000, 27999], [1, 0], 2),
+    (20000, 648, 1288, 63, [0, 19990], [2], 3),
+    (20000, 648, 1288, 33, [0, 10000, 20000], [1, 0], 2),
+    (20000, 648, 1288, 17, [0, 20000], [0], 1),
+    (30000, 640, 640, 5, [9, 15000, 30000], [0, 1], 2),
+]
+
+
+def backward_by_tiles(shape, xt, wt, dx=True, base=True):
+    M, K, N, R, cuts, _, G = shape
+    return fpq.fpq_adapter_backward_route(M, N, K, G, R, len(cuts) - 1, KIND[xt], KIND[wt], dx, base) == fpq.ADAPTER_TILES
+
+
+def test_the_backward_route_is_that_of_padded_weights():
+    for xt, wt in A.TYPES:
+        for K, N in ((1280, 640), (648, 1288)):
+            for R in (12, 18, 20, 28, 36, 60):
+                for dx, base in ((True, True), (True, False), (False, False)):
+                    shape = (32768, K, N, R, [0, 32768], [0], 1)
+                    padded = shape[:3] + (-(-R // 8) * 8,) + shape[4:]
+                    assert backward_by_tiles(shape, xt, wt, dx, base) == backward_by_tiles(padded, xt, wt, dx, base)
+                assert backward_by_tiles(padded, xt, wt) == (fpq.fpq_adapter_route(32768, K, N, 1, padded[3], 1, KIND[xt], KIND[wt]) == fpq.ADAPTER_TILES)
+    for xt, wt in A.TYPES:                                 # every type and padded rank is among the cases below
+        ranks = {max(16, 1 << (s[3] - 1).bit_length()) for s in TALL_ODD_RANKS if backward_by_tiles(s, xt, wt)}
+        assert ranks >= ({32, 64} if xt == F32 else {16, 32, 64})
+    with pytest.raises(fpq.FpqError, match="shape"):
+        fpq.fpq_adapter_backward_route(1, 1, 1, 1, 200, 1, fpq.FP32, fpq.FP32)
+    with pytest.raises(fpq.FpqError, match="unsupported"):
+        fpq.fpq_adapter_backward_route(1, 1, 1, 1, 2, 1, fpq.BF16, fpq.FP32)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("xt,wt", A.TYPES)
+@pytest.mark.parametrize("shape", TALL_ODD_RANKS, ids=lambda s: "x".join(map(str, s[:4])))
+def test_tall_backward_of_ranks_that_are_padded(shape, xt, wt):
+    t = A.make(*shape, xt=xt, wt=wt)
+    M, K, R = t["x"].shape[0], t["x"].shape[1], t["a"].shape[1]
+    u = torch.randn(M, R, device="cuda")
+    dx = torch.full((M, K), -7.0, dtype=xt, device="cuda")
+    before = dx.clone()
+    A.check_backward(t, u, *backward(t, u, base=t["dbase"], dx=dx), before)
+    _, da, db = backward(t, u, need_dx=False)
+    A.check_backward(t, u, None, da, db, None, have_dx=False)
+    A.check_forward(t, *A.run_forward(t))
+    assert fpq.fpq_read_status() == fpq.OK
