@@ -434,11 +434,13 @@ fpq_status fpq_round_learn_harden(const float* alpha, int64_t N, int64_t K, uint
  *   offsets  [S + 1] int32, non-decreasing (values outside 0 .. M are clamped: a wrong list gives wrong rows, no access
  *            out of range); ids [S] int32.  One adapter may serve any number of segments; segments may be empty
  *   u        NULL, or [M][R] FP32 out: what fpq_adapter_backward reads
- * Sums are FP32: FP32 operands enter the tensor cores as two TF32 terms each (errors of 2^-22 of the sum of absolute
- * terms, as FP32 multiply-adds have; the second term of a number below 2^-114 is subnormal and counts as zero: 2^-11 of it can be
- * lost), 16-bit operands as they are (with BF16, t in two terms: 2^-18 of it is left out); y is rounded once.  An infinite or NaN
- * operand gives what FP32 multiply-adds give.  A row's result depends on its own values, its adapter, and the sizes and alignment of
- * the call alone, and equal calls give equal bits.
+ * Sums are FP32.  FP32 operands enter the tensor cores as two TF32 terms each (2^-20 of a product three times: what the product of the
+ * second terms and their own ends leave out; the second term of a number below 2^-114 is subnormal and counts as zero: 2^-11 of it
+ * can be lost), 16-bit operands as they are (with BF16, t in two terms: 2^-18 of it is left out), and the tensor cores cut their sums
+ * off instead of rounding them.  At most, then, u is off by FPQ_ADAPTER_ERROR(K / 64) of the sum of its absolute terms
+ * sum |A| |x|; y by FPQ_ADAPTER_ERROR(K / 64) + 2^-16 of |scale| sum |B| |A| |x| and its roundings, to FP32 with base and to its type.
+ * (Seen: 2^-18 with numbers of one sign and nearly full mantissas.)  An infinite or NaN operand gives what FP32 multiply-adds give.  A row's result
+ * depends on its own values, its adapter, and the sizes and alignment of the call alone, and equal calls give equal bits.
  *
  * fpq_adapter_backward: the gradients, from dy [M][N] (rows ld_dy apart) and what forward read and kept:
  *     t[i] = scale[g] * B[g]^T dy[i],   dx[i] = base[i] + A[g]^T t[i],
@@ -447,6 +449,8 @@ fpq_status fpq_round_learn_harden(const float* alpha, int64_t N, int64_t K, uint
  *   dx       [M][K] out, or NULL when x needs no gradient; rows in no segment stay as they were
  *   da, db   [G][R][K] and [G][N][R] FP32 out, overwritten (zeros for an adapter without rows).  No atomics: equal calls
  *            give equal bits
+ * t and dx are off by as much as u and y, with N for K and dy for x; db by FPQ_ADAPTER_ERROR(rows / 32) of |scale| sum |dy| |u|, da by
+ * FPQ_ADAPTER_ERROR(rows / 32) + FPQ_ADAPTER_ERROR(N / 64) of |scale| sum |B| |dy| |x| over the adapter's rows.
  *   workspace  fpq_adapter_backward_workspace_size bytes (0 for sizes out of range), 16-byte aligned, contents not kept; not for two
  *            calls at once
  * One kernel forward, three or four backward, on `stream`; no allocation, no synchronisation.  Pointers are aligned to their
@@ -454,6 +458,7 @@ fpq_status fpq_round_learn_harden(const float* alpha, int64_t N, int64_t K, uint
  * up to 2^24, G up to 65535, G * R * max(N, K) below 2^40, G * (N + K) below 2^33.  M = 0 or S = 0: forward does nothing, backward writes zeros to
  * da and db.  Errors: FPQ_ERR_UNSUPPORTED, FPQ_ERR_SHAPE, FPQ_ERR_NULL, FPQ_ERR_ALIGN, FPQ_ERR_WORKSPACE, FPQ_ERR_CUDA.
  */
+#define FPQ_ADAPTER_ERROR(n) ((68.0 + (n)) / 8388608.0)
 enum { FPQ_FP32 = 0, FPQ_BF16 = 1, FPQ_FP16 = 2, FPQ_E4M3_BLOCK32 = 3 };
 fpq_status fpq_adapter_forward(const void* x, int64_t ldx, int32_t x_type, const void* a, const void* b, int32_t w_type,
                                const float* scale, int32_t G, int32_t R, const int32_t* offsets, const int32_t* ids, int32_t S,

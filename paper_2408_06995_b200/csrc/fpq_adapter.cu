@@ -18,9 +18,10 @@
 // overlap (weights transposed, rows, gradients): of a small call's 13 us most is their latency.
 //
 // Products run on the tensor cores as TF32 with FP32 operands in two terms x = hi + lo of 11 significant bits each: hi hi, hi lo and
-// lo hi (16-bit operands are TF32 numbers themselves, one term, or are multiplied as they are).  Some 2^-22 of a product is left
-// out.  The tensor cores cut their sums off instead of rounding them: at most 64 columns, or 16 rows, are summed there, the rest in
-// registers by FP32 additions.  The order of a reduction is free: a thread's share of a row lies side by side.
+// lo hi (16-bit operands are TF32 numbers themselves, one term, or are multiplied as they are).  Up to 2^-20 of a product is left
+// out: 2^-22 are lo lo, 2^-21 each what the tensor core does not read of either lo.  The tensor cores cut their sums off instead of
+// rounding them: at most 64 columns, 16 rows, or the up to 128 ranks of an output (48 MMAs) are summed there, the rest in registers by
+// FP32 additions.  The order of a reduction is free: a thread's share of a row lies side by side.
 //
 // An infinity, or a number that rounds up to one, has no split: a result that is not finite is worked out again by FP32
 // multiply-adds.

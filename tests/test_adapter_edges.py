@@ -1,9 +1,13 @@
 """Adapters at sizes, alignments and values where their parts meet: against the formulas in 64 bits."""
+import os
+import re
+
 import pytest
 import torch
 
 import paper_2408_06995_b200 as fpq
 import test_adapters as A
+from paper_2408_06995_b200 import build as fpq_build
 
 F32, BF, HF = torch.float32, torch.bfloat16, torch.float16
 KIND = {F32: fpq.FP32, BF: fpq.BF16, HF: fpq.FP16}
@@ -147,3 +151,62 @@ def test_tall_backward_of_ranks_that_are_padded(shape, xt, wt):
     A.check_backward(t, u, None, da, db, None, have_dx=False)
     A.check_forward(t, *A.run_forward(t))
     assert fpq.fpq_read_status() == fpq.OK
+
+
+# ---- the documented bounds --------------------------------------------------------------------------------------------
+
+def documented():
+    """FPQ_ADAPTER_ERROR as the header has it."""
+    text = open(os.path.join(fpq_build.ROOT, "include", "fpq.h")).read()
+    add, unit = re.search(r"#define FPQ_ADAPTER_ERROR\(n\) \(\(([\d.]+) \+ \(n\)\) / ([\d.]+)\)", text).groups()
+    return lambda n: (float(add) + n) / float(unit)
+
+
+def test_the_documented_bounds_hold_what_the_terms_add_up_to():
+    """Units of 2^-23.  Operands: 2^-20 three times, 24.  t: up to 24 sums cut off inside the tensor cores (64 FP32 columns: eight MMAs of
+    three products), then K / 64 FP32 additions and up to 20 of warps and blocks.  y: 3 R / 8 sums inside, and 2^-18 of t beside BF16
+    weights.  Gradients: a sum of 8 rows at a time and warp, two warps at least, each addition rounded by half a unit."""
+    bound = documented()
+    for D in (1, 64, 1280, 1 << 24):
+        assert bound(D / 64) >= A.product_error(D, 24) >= 2.0 ** -24
+        assert bound(D / 32) >= 3 * 2.0 ** -20 + (24 + 20 + D / 16 / 2) * 2.0 ** -23
+    for R in (1, 128):
+        assert 2.0 ** -16 >= A.product_error(R, 3 * R / 8) + 2.0 ** -23 + 2.0 ** -18
+
+
+def full(shape, dtype, g):
+    """Positive numbers in [0.5, 4) whose every mantissa bit but a few is set: the longest remainders of every split, and sums that are cut off
+    towards one side throughout."""
+    bits = {F32: 23, BF: 7, HF: 10}[dtype]
+    m = (1 << bits) - 1 - (torch.randint(0, 8, shape, generator=g, device="cuda") << torch.randint(0, bits - 2, shape, generator=g, device="cuda")) % (1 << bits)
+    return ((1 + m.double() / (1 << bits)) * 2.0 ** torch.randint(-1, 2, shape, generator=g, device="cuda").double()).to(dtype)
+
+
+BOUNDED = [(1, 1280, 640, 16), (300, 1280, 320, 128), (257, 96, 2560, 128), (3000, 320, 96, 24), (9000, 640, 1288, 64), (20000, 640, 1288, 32),
+           (30000, 328, 648, 60), (70000, 64, 32, 128), (12000, 2560, 64, 64)]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("xt,wt", A.TYPES)
+@pytest.mark.parametrize("M,K,N,R", BOUNDED)
+def test_the_documented_bounds(M, K, N, R, xt, wt):
+    g = torch.Generator(device="cuda").manual_seed(M)
+    bound = documented()
+    x, dy, a, b, u0 = full((M, K), xt, g), full((M, N), xt, g), full((1, R, K), wt, g), full((1, N, R), wt, g), full((M, R), F32, g)
+    if xt == HF:                                           # (sums that its range holds)
+        a, b = a * 2.0 ** -8, b * 2.0 ** -10
+    s = 1.2345678806304932
+    scale, offsets, ids = torch.tensor([s], device="cuda"), torch.tensor([0, M], dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    u = torch.empty(M, R, device="cuda")
+    y = fpq.fpq_adapter_forward(x, a, b, offsets, ids, scale, None, None, u)
+    dx, da, db = fpq.fpq_adapter_backward(dy, x, u0, a, b, offsets, ids, scale)
+    x, dy, a, b, u0 = x.double(), dy.double(), a[0].double(), b[0].double(), u0.double()
+    ue, te = x @ a.T, s * (dy @ b)                         # (everything is positive: each sum is that of its absolute terms)
+    second = 2.0 ** -16
+    for name, got, want, error in (("u", u, ue, bound(K / 64)), ("y", y, s * (ue @ b.T), bound(K / 64) + second), ("dx", dx, te @ a, bound(N / 64) + second),
+                                   ("da", da[0], te.T @ x, bound(M / 32) + bound(N / 64)), ("db", db[0], s * (dy.T @ u0), bound(M / 32))):
+        assert bool(torch.isfinite(got).all())
+        off = (got.double() - want).abs()
+        allowed = error * want + A.half_step(got.dtype, want * (1 + error)) + 2.0 ** -24 * want
+        worst = float((off / allowed).max())
+        assert worst <= 1, (name, worst)
