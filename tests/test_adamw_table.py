@@ -1,8 +1,13 @@
 """The AdamW step's table and roots, apart from the step itself."""
+import ctypes
+import os
+import subprocess
+
 import pytest
 import torch
 
 import paper_2408_06995_b200 as fpq
+from paper_2408_06995_b200 import build as fpq_build
 
 F32, BF = torch.float32, torch.bfloat16
 
@@ -60,3 +65,43 @@ def test_the_table_takes_buffers_side_by_side(codes):
 def test_the_table_refuses_memory_in_two_roles(codes, changed):
     with pytest.raises(AssertionError, match="overlap|twice"):
         memory_table(codes, **changed)
+
+
+ROOTS = r"""#include <stdint.h>
+
+#include "fpq_roots.cuh"
+
+// Counts the numbers of [first, last) (as bits) whose roots are not those rounded to nearest, and keeps the smallest of them.
+__global__ void compare(uint32_t first, uint32_t last, unsigned long long* wrong, unsigned* smallest)
+{
+    for (uint64_t i = first + 2ull * (blockIdx.x * blockDim.x + threadIdx.x); i < last; i += 2ull * gridDim.x * blockDim.x) {
+        const float2 v = make_float2(__uint_as_float((uint32_t)i), __uint_as_float(i + 1 < last ? (uint32_t)i + 1 : first));
+        const float2 r = fpq::roots_of(v);
+        if (__float_as_uint(r.x) != __float_as_uint(__fsqrt_rn(v.x)) || __float_as_uint(r.y) != __float_as_uint(__fsqrt_rn(v.y))) {
+            atomicAdd(wrong, 1ull);
+            atomicMin(smallest, (unsigned)i);
+        }
+    }
+}
+
+extern "C" int roots(uint32_t first, uint32_t last, unsigned long long* wrong, unsigned* smallest, void* stream)
+{
+    compare<<<148 * 8, 256, 0, (cudaStream_t)stream>>>(first, last, wrong, smallest);
+    return (int)cudaGetLastError();
+}
+"""
+
+
+@pytest.mark.gpu
+def test_roots_are_rounded_to_nearest(tmp_path):
+    """Every FP32 number from 2^-96 to the largest, and zero: what the step uses without a branch."""
+    (tmp_path / "roots.cu").write_text(ROOTS)
+    so = tmp_path / "roots.so"
+    subprocess.run([os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc"), "-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-std=c++17", "-shared",
+                    "-Xcompiler", "-fPIC", "-cudart", "static", "-I", fpq_build.CSRC, str(tmp_path / "roots.cu"), "-o", str(so)], check=True)
+    f = ctypes.CDLL(str(so)).roots
+    f.argtypes = [ctypes.c_uint32, ctypes.c_uint32] + [ctypes.c_void_p] * 3
+    for first, last in ((0, 1), ((127 - 96) << 23, 0x7F800000)):
+        wrong, smallest = torch.zeros(1, dtype=torch.int64, device="cuda"), torch.full((1,), 0x7FFFFFFF, dtype=torch.int32, device="cuda")
+        assert f(first, last, wrong.data_ptr(), smallest.data_ptr(), torch.cuda.current_stream().cuda_stream) == 0
+        assert int(wrong) == 0, f"{int(wrong)} wrong, from bits {int(smallest):#x} on"
