@@ -435,12 +435,13 @@ fpq_status fpq_round_learn_harden(const float* alpha, int64_t N, int64_t K, uint
  *            out of range); ids [S] int32.  One adapter may serve any number of segments; segments may be empty
  *   u        NULL, or [M][R] FP32 out: what fpq_adapter_backward reads
  * Sums are FP32.  FP32 operands enter the tensor cores as two TF32 terms each (2^-20 of a product three times: what the product of the
- * second terms and their own ends leave out; the second term of a number below 2^-114 is subnormal and counts as zero: 2^-11 of it
- * can be lost), 16-bit operands as they are (with BF16, t in two terms: 2^-18 of it is left out), and the tensor cores cut their sums
- * off instead of rounding them.  At most, then, u is off by FPQ_ADAPTER_ERROR(K / 64) of the sum of its absolute terms
- * sum |A| |x|; y by FPQ_ADAPTER_ERROR(K / 64) + 2^-16 of |scale| sum |B| |A| |x| and its roundings, to FP32 with base and to its type.
- * (Seen: 2^-18 with numbers of one sign and nearly full mantissas.)  An infinite or NaN operand gives what FP32 multiply-adds give.  A row's result
- * depends on its own values, its adapter, and the sizes and alignment of the call alone, and equal calls give equal bits.
+ * second terms and their own ends leave out), 16-bit operands as they are (with BF16, t in two terms: 2^-18 of it is left out), and the
+ * tensor cores cut their sums off instead of rounding them.  At most, then, u is off by FPQ_ADAPTER_ERROR(K / 64) of the sum of its
+ * absolute terms sum |A| |x|; y by FPQ_ADAPTER_ERROR(K / 64) + 2^-16 of |scale| sum |B| |A| |x| and its roundings, to FP32 with
+ * base and to its type.  (Seen: 2^-18 with numbers of one sign and nearly full mantissas.)  Besides, up to 2^-133 of each FP32
+ * operand, t and u among them, is lost: numbers below 2^-110 have fewer bits, those below 2^-133 may count as zero.  An infinite or NaN
+ * operand gives what FP32 multiply-adds give.  A row's result depends on its own values, its adapter, and the sizes and alignment of
+ * the call alone, and equal calls give equal bits.
  *
  * fpq_adapter_backward: the gradients, from dy [M][N] (rows ld_dy apart) and what forward read and kept:
  *     t[i] = scale[g] * B[g]^T dy[i],   dx[i] = base[i] + A[g]^T t[i],

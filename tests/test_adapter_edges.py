@@ -210,3 +210,40 @@ def test_the_documented_bounds(M, K, N, R, xt, wt):
         allowed = error * want + A.half_step(got.dtype, want * (1 + error)) + 2.0 ** -24 * want
         worst = float((off / allowed).max())
         assert worst <= 1, (name, worst)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("xt,wt", [(F32, F32), (F32, BF), (BF, BF)])
+@pytest.mark.parametrize("M,K,N,R", [(64, 128, 96, 16), (20000, 640, 1280, 32)])
+@pytest.mark.parametrize("x_exp,a_exp,b_exp,dy_exp,u_exp", [(-112, 10, 10, 0, 0), (-130, 20, 10, -118, 5), (-145, 30, 30, -130, 20), (10, -130, 20, 10, -125), (0, 20, -130, 5, -140), (-70, -75, 0, -40, -40),
+                                                          (-100, -40, 10, -140, 30)])
+def test_operands_near_the_smallest_numbers(M, K, N, R, x_exp, a_exp, b_exp, dy_exp, u_exp, xt, wt):
+    """What is lost of an FP32 operand lies below 2^-133, and sums end at FP32's 2^-149 (each cut-off addition, up to three for 8 terms)."""
+    bound, lost, least = documented(), 2.0 ** -133, 2.0 ** -149
+    g = torch.Generator(device="cuda").manual_seed(M)
+
+    def numbers(shape, exponent, dtype):
+        return ((1 + torch.rand(shape, generator=g, device="cuda", dtype=torch.float64)) * 2.0 ** exponent).to(F32).to(dtype)
+
+    x, a, b, dy, u0 = numbers((M, K), x_exp, xt), numbers((1, R, K), a_exp, wt), numbers((1, N, R), b_exp, wt), numbers((M, N), dy_exp, xt), numbers((M, R), u_exp, F32)
+    offsets, ids = torch.tensor([0, M], dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    u = torch.empty(M, R, device="cuda")
+    y = fpq.fpq_adapter_forward(x, a, b, offsets, ids, None, None, None, u)
+    dx, da, db = fpq.fpq_adapter_backward(dy, x, u0, a, b, offsets, ids)
+    x, a, b, dy, u0 = x.double(), a[0].double(), b[0].double(), dy.double(), u0.double()
+
+    def product(p, q, p_off, q_off, error):
+        """p q^T, and how far it may be off when p and q are."""
+        D = p.shape[1]
+        return p @ q.T, (error * p + p_off) @ q.T + (p + p_off).sum(1, keepdim=True) * q_off + D * least
+
+    x_off, w_off = lost if xt == F32 else 0.0, lost if wt == F32 else 0.0
+    ue, u_off = product(x, a, x_off, w_off, bound(K / 64))
+    ye, y_off = product(ue, b, u_off + lost, w_off, 2.0 ** -16)
+    te, t_off = product(dy, b.T, x_off, w_off, bound(N / 64))
+    xe, dx_off = product(te, a.T, t_off + lost, w_off, 2.0 ** -16)
+    ae, da_off = product(te.T, x.T, (t_off + lost).T, x_off, bound(M / 32))
+    be, db_off = product(dy.T, u0.T, torch.full_like(dy.T, x_off), lost, bound(M / 32))
+    for name, got, want, off in (("u", u, ue, u_off), ("y", y, ye, y_off), ("dx", dx, xe, dx_off), ("da", da[0], ae, da_off), ("db", db[0], be, db_off)):
+        allowed = off + A.half_step(got.dtype, want + off) + 2.0 ** -24 * want
+        assert bool(((got.double() - want).abs() <= allowed).all()), (name, float(((got.double() - want).abs() / allowed).max()))
