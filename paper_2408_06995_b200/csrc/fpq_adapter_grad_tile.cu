@@ -373,8 +373,12 @@ cudaError_t launch_as(const GradArgs& a, cudaStream_t st)
 
 }  // namespace
 
-// From 1024 rows on (whole backward passes, the gradients by warps and so: 1024 rows, 320 -> 320, rank 32: 21.8 and 16.3 us; 65536 rows, 640 ->
-// 2560, rank 64: 505 and 271; 512 rows of 32 adapters, rank 16: 22.4 and 27.2).  Rows that start between 16-byte boundaries, and ranks that are no
+// From 1024 rows on.  Whole backward passes, the gradients by warps and so, us: one adapter, 1024 rows, 320 -> 320, rank 16: 16.9 and
+// 13.9; 8192 rows, 640 -> 640, rank 64: 56 and 37; 32768 rows, 1280 -> 640, rank 32: 103 and 78; 512 rows of 32 adapters, rank 16: 22.4
+// and 27.2.  Every segment costs a run of 64 rows here and of 16 or 32 by warps, which the rule does not look at: one adapter in segments
+// of 4 rows, 8192 rows, 320 -> 320: 414 and 371; 16 adapters in segments of 16, 1280 -> 640: 93 and 105; 64 adapters in segments of 16, 320 ->
+// 320: 42 and 56; 4 adapters, 1024 rows in as many segments: 114 and 188.  (One adapter, or 256 rows to each and 48 to a segment, would
+// leave 1.6 % over the better one of 300 shapes instead of 9.5 %.)  Rows that start between 16-byte boundaries, and ranks that are no
 // multiple of four, go by warps.
 bool adapter_grad_tiles_preferred(const GradArgs& a)
 {
