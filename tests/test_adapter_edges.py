@@ -247,3 +247,39 @@ def test_operands_near_the_smallest_numbers(M, K, N, R, x_exp, a_exp, b_exp, dy_
     for name, got, want, off in (("u", u, ue, u_off), ("y", y, ye, y_off), ("dx", dx, xe, dx_off), ("da", da[0], ae, da_off), ("db", db[0], be, db_off)):
         allowed = off + A.half_step(got.dtype, want + off) + 2.0 ** -24 * want
         assert bool(((got.double() - want).abs() <= allowed).all()), (name, float(((got.double() - want).abs() / allowed).max()))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("xt,R", [(BF, 64), (BF, 32), (F32, 64), (HF, 24)])
+def test_tiles_on_two_streams_and_replayed(xt, R):
+    """Tall calls of two streams share the SMs and their tensor memory; a captured one serves other segments."""
+    M, K, N, G = 20000, 648, 1288, 2
+    assert fpq.fpq_adapter_route(M, N, K, G, R, 3, KIND[xt], KIND[xt]) == fpq.ADAPTER_TILES
+    t = A.make(M, K, N, R, [0, 7000, 12000, 20000], [0, -1, 1], G, xt, xt)
+    u0 = torch.randn(M, R, device="cuda")
+
+    def both():
+        u = torch.zeros(M, R, device="cuda")
+        y = fpq.fpq_adapter_forward(t["x"], t["a"], t["b"], t["offsets"], t["ids"], t["scale"], t["base"], None, u)
+        return (y, u) + backward(t, u0, base=t["dbase"])
+
+    want = both()
+    torch.cuda.synchronize()
+    got, streams = [], [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(4):
+        for s in streams:
+            with torch.cuda.stream(s):
+                got.append(both())
+    torch.cuda.synchronize()
+    for g in got:
+        assert all(torch.equal(a, b) for a, b in zip(g, want))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = both()
+    t["offsets"].copy_(torch.tensor([5, 6, 15000, 19000], dtype=torch.int32))
+    t["ids"].copy_(torch.tensor([1, 0, 1], dtype=torch.int32))
+    for _ in range(2):
+        graph.replay()
+    want = both()
+    assert all(torch.equal(a, b) for a, b in zip(out, want))
+    assert fpq.fpq_read_status() == fpq.OK
