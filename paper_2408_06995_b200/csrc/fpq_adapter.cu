@@ -204,7 +204,8 @@ struct RowsRing {
 };
 
 // A block has 16 * wr rows; each of its warps takes 16 of them and, with the 8 / wr warps (times the blocks of the cluster) that
-// have the same rows, shares the reduction in groups of 32 columns, then the output in groups of 32 columns.  RP: the rank, padded.
+// have the same rows, shares the reduction in groups of 32 columns, then the output in groups of 32 columns.  RP: the rank, padded.  (Two blocks on an
+// SM leave 128 registers: rank 64 spills 180 bytes with FP32 rows and weights, 280 without vectors, 16 to 108 otherwise.)
 template <typename XT, typename WT, int RP, bool VEC>
 __global__ void __launch_bounds__(THREADS, RP <= 64 ? 2 : 1) adapter_rows_kernel(const RowsArgs a)
 {
@@ -616,7 +617,8 @@ struct GradRing {
     static constexpr int STAGES = sizeof(XT) == 2 && JT == 32 ? 3 : 2;                            // two blocks on an SM
 };
 
-// JT: ranks of a warp; RP / JT warps share a run of rows.
+// JT: ranks of a warp; RP / JT warps share a run of rows.  (Two blocks on an SM leave 128 registers: FP32 rows spill 116 to 140 bytes, FP16 20
+// to 44, BF16 4 to 16.)
 template <typename XT, int RP, int JT>
 __global__ void __launch_bounds__(THREADS, 2) adapter_grad_kernel(const GradArgs a)
 {

@@ -11,7 +11,7 @@
 //      them (the rows of a request's last tile, which are fewer, are stored by the warp).
 // Bound by memory: 18944 x 64 -> 2560, BF16, rank 64, one block for every SM: 44 us, 4.4 TB/s; the pass by warps (fpq_adapter.cu), which
 // spends some 300 instructions on 16 x 32 values, 95 us.  A wave of blocks has some 7 us of its own (finding the tile, the first copies,
-// the step from t to y).  32768 x 320 -> 2560, two blocks on an SM: 76 us against 159.
+// the step from t to y).  32768 x 320 -> 2560, two blocks on an SM: 76 to 80 us against 159.
 #include <math.h>
 
 #include <algorithm>
