@@ -20,7 +20,7 @@
 // Products run on the tensor cores as TF32 with FP32 operands in two terms x = hi + lo of 11 significant bits each: hi hi, hi lo and
 // lo hi (16-bit operands are TF32 numbers themselves, one term, or are multiplied as they are).  Up to 2^-20 of a product is left
 // out: 2^-22 are lo lo, 2^-21 each what the tensor core does not read of either lo.  The tensor cores cut their sums off instead of
-// rounding them: at most 64 columns, 16 rows, or the up to 128 ranks of an output (48 MMAs) are summed there, the rest in registers by
+// rounding them: at most 64 columns, 16 rows or 64 ranks (24 MMAs) are summed there, with BF16 rows 128 ranks, the rest in registers by
 // FP32 additions.  The order of a reduction is free: a thread's share of a row lies side by side.
 //
 // An infinity, or a number that rounds up to one, has no split: a result that is not finite is worked out again by FP32
@@ -496,12 +496,20 @@ __global__ void __launch_bounds__(THREADS, RP <= 64 ? 2 : 1) adapter_rows_kernel
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
                             w[e].values(f[e]);
+                        // (above 64 ranks the sums of 32 are added in registers: cut off throughout, y was 1.1e-6 off instead of 0.4e-6)
+                        float part[RP > 64 ? 4 : 1][4] = {};
 #pragma unroll
                         for (int st = 0; st < TPER / 2; ++st) {
                             const float v[4][2] = {{f[0][2 * st], f[0][2 * st + 1]}, {f[1][2 * st], f[1][2 * st + 1]},
                                                    {f[2][2 * st], f[2][2 * st + 1]}, {f[3][2 * st], f[3][2 * st + 1]}};
-                            mma_split<true, WIDE<WT>, 4>(acc, h[st], l[st], v);
+                            mma_split<true, WIDE<WT>, 4>(RP > 64 ? part : acc, h[st], l[st], v);
                         }
+                        if constexpr (RP > 64)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                                for (int k = 0; k < 4; ++k)
+                                    acc[e][k] += part[e][k];
                     }
                 }
                 float zero = 0.f;                          // becomes NaN if a sum is not finite
