@@ -438,7 +438,7 @@ fpq_status fpq_round_learn_harden(const float* alpha, int64_t N, int64_t K, uint
  * second terms and their own ends leave out), 16-bit operands as they are (with BF16, t in two terms: 2^-18 of it is left out), and the
  * tensor cores cut their sums off instead of rounding them.  At most, then, u is off by FPQ_ADAPTER_ERROR(K / 64) of the sum of its
  * absolute terms sum |A| |x|; y by FPQ_ADAPTER_ERROR(K / 64) + 2^-16 of |scale| sum |B| |A| |x| and its roundings, to FP32 with
- * base and to its type.  (Seen: 2^-18 with numbers of one sign and nearly full mantissas.)  Besides, up to 2^-133 of each FP32
+ * base and to its type.  (Seen: 2^-19 with numbers of one sign and nearly full mantissas.)  Besides, up to 2^-133 of each FP32
  * operand, t and u among them, is lost: numbers below 2^-110 have fewer bits, those below 2^-133 may count as zero.  An infinite or NaN
  * operand gives what FP32 multiply-adds give.  A row's result depends on its own values, its adapter, and the sizes and alignment of
  * the call alone, and equal calls give equal bits.
