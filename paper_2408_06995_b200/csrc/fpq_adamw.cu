@@ -7,7 +7,7 @@
 // ones.  One kernel goes once over all tensors: runs of 1024 or 2048 elements of one tensor, found in the list that travels in
 // the kernel's arguments, go round the blocks that the SMs hold.  The blocks work the bias corrections out themselves from the
 // step count on the device, so a captured launch can be replayed; the last block to have read the count moves it on.
-// FP32 moments: 6.2 M elements in 256 tensors 36 us, 5.2 TB/s.  8-bit moments: 73.7 M elements 294 us, 4.0 TB/s (257 with a part of them in
+// FP32 moments: 6.2 M elements in 256 tensors 36 us, 5.2 TB/s.  8-bit moments: 73.7 M elements 281 to 295 us, 4.1 TB/s (257 with a part in
 // the L2), of which the issue of 97 instructions per element takes 202 at 1.87 GHz; 73 % of the issue slots are used; warps wait
 // for arithmetic pipes and fixed latencies, hardly for memory.  The same 256 tensors 32 us.
 //
